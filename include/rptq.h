@@ -9,8 +9,8 @@
  *                           cluster segment on the tensor cores, floating-point epilogue (calls
  *                           with at most 16 tokens run a second kernel with the same arithmetic)
  * Further down: the same product with per-cluster asymmetric weights or as a de-quantised
- * bfloat16 product, attention on quantised Q / K / V, calibration on the device, and aids for
- * tests and measurement.
+ * bfloat16 product, attention on quantised Q / K / V, the paged key / value cache with its attention,
+ * calibration on the device, and aids for tests and measurement.
  *
  * Conventions
  *   - Every function returns an int status: RPTQ_OK or a negative RPTQ_ERR_* value. Nothing
@@ -18,7 +18,7 @@
  *   - "dev" pointers are device global memory of the device that was current when the layout
  *     was created; "host" pointers are ordinary host memory. The caller owns every buffer. The
  *     library allocates device memory only inside rptq_layout_create (small tables, and with a
- *     device's first layout one status word).
+ *     device's first layout one status word) and rptq_kv_cache_create (small tables).
  *   - Kernel launches are asynchronous on `stream` (a cudaStream_t passed as void*; NULL is the
  *     default stream). A layout handle is immutable after creation and may be used from several
  *     streams at once.
@@ -80,7 +80,8 @@ enum {
     RPTQ_ERR_NOT_BIJECTION = -3,   /* perm is not a permutation of 0..C-1, or sizes do not sum to C */
     RPTQ_ERR_CUDA = -4,            /* a CUDA runtime or driver call failed */
     RPTQ_ERR_DEVICE_TIMEOUT = -5,  /* a bounded wait inside a kernel ran out (see rptq_get_device_status) */
-    RPTQ_ERR_ALLOC = -6            /* host or device allocation failed */
+    RPTQ_ERR_ALLOC = -6,           /* host or device allocation failed */
+    RPTQ_ERR_BAD_SLOT = -7         /* a slot or page past the end of the pool (see rptq_get_device_status) */
 };
 
 enum { RPTQ_OUT_F32 = 0, RPTQ_OUT_F16 = 1, RPTQ_OUT_CODES = 2 };
@@ -88,7 +89,11 @@ enum { RPTQ_ACT_NONE = 0, RPTQ_ACT_RELU = 1 };
 enum { RPTQ_FORMAT_VERSION = 2 };
 enum { RPTQ_ORDER_CONTIGUOUS = 0, RPTQ_ORDER_INTERLEAVED = 1 };
 
+/* element types of rows that a caller hands over or takes back (rptq_kv_cache_write / _read, rptq_attention_paged) */
+enum { RPTQ_ROWS_F32 = 0, RPTQ_ROWS_F16 = 1, RPTQ_ROWS_CODES = 2, RPTQ_ROWS_BF16 = 3 };
+
 typedef struct rptq_layout rptq_layout_t;
+typedef struct rptq_kv_cache rptq_kv_cache_t;
 
 /*
  * Sec. 4.1: the reorder index S (concatenated cluster index sets) with one (s_c, z_c) per
@@ -285,8 +290,8 @@ int64_t rptq_weight_codes_bytes(int K_pad, int64_t N_pad);
 
 /*
  * Kernels never spin without a limit: a wait that runs out records RPTQ_ERR_DEVICE_TIMEOUT in a
- * device status word, lets the block drain and return, and leaves the output undefined. This call
- * synchronises the current device, returns the current context's word in *status (RPTQ_OK if
+ * device status word, lets the block drain and return, and leaves the output undefined. A slot or page that lies
+ * outside its pool records RPTQ_ERR_BAD_SLOT there. This call synchronises the current device, returns the current context's word in *status (RPTQ_OK if
  * nothing happened) and clears it. Each device has its own word, and each further context of it.
  */
 int rptq_get_device_status(int* status);
@@ -391,6 +396,69 @@ int rptq_attention(const rptq_layout_t* LQ, const rptq_layout_t* LK, const rptq_
 int rptq_attention_kv(const rptq_layout_t* LK, const rptq_layout_t* LV, int n_heads,
                       const void* q_f16, int64_t ldq, int Tq, const void* k_codes, const void* v_codes, int Tk, int n_seq,
                       float qk_scale, int causal, void* out_f16, int64_t ldo, void* stream);
+
+/*
+ * The paged key / value cache of a server (Sec. 5.2; the paper quantises the cache, it has no pages): sequences of different
+ * lengths that grow by a token a step, in pages handed out from a pool. Keys and values are quantised as they are written
+ * (rptq_kv_cache_write), can be read back (rptq_kv_cache_read), and rptq_attention_paged attends over them.
+ *
+ * A handle describes a cache; the caller owns the pools and hands out the pages.
+ *   LK, LV     the layouts of the attention sites, as for rptq_attention_kv (3, 4 or 8 bits each); their cluster parameters are
+ *              copied. Only which channel has which (s_c, z_c) matters here: any reorder index and unit order will do
+ *   n_heads    heads of the cache; head h owns the channels h * d .. (h + 1) * d - 1, d = C / n_heads <= 256
+ *   page_size  keys per page, a multiple of 16, at most 65536
+ * A pool is n_pages pages of k_page_bytes (v_page_bytes) bytes, one after the other, 16-byte aligned. Slot s is key s % page_size of page
+ * s / page_size. The bytes inside a page are the library's choice (format version 2): channels in their own order, a head's rounded up
+ * to a multiple of 32, so a page takes page_size * n_heads * roundup32(d) * bits / 8 bytes.
+ * rptq_kv_cache_destroy frees the handle; work that uses it must have completed. NULL is OK.
+ */
+int rptq_kv_cache_create(rptq_kv_cache_t** out, const rptq_layout_t* LK, const rptq_layout_t* LV, int n_heads, int page_size);
+int rptq_kv_cache_query(const rptq_kv_cache_t* cache, int64_t* k_page_bytes, int64_t* v_page_bytes);
+int rptq_kv_cache_destroy(rptq_kv_cache_t* cache);
+
+/*
+ * Quantise on write: for token i and channel ch of cluster c,
+ *   q = clamp(rne(x[i][ch] / s_c) + z_c, 0, 2^bits - 1)
+ * with x / s_c as the exact product of x and (float)(1.0/(double)s_c), rounded once (as rptq_ln_reorder_quant does), into slot slots[i].
+ *   k, v       dev, n_tokens rows of C elements of rows_type, ldk / ldv elements apart (original channel order). NaN gives code 0.
+ *              RPTQ_ROWS_CODES: packed code rows of LK / LV (as rptq_cluster_gemm writes them with RPTQ_OUT_CODES),
+ *              ldk / ldv bytes apart (multiples of 4); the codes are moved as they are
+ *   slots      dev int64 [n_tokens]. A negative slot: the token is skipped. A slot >= n_pages * page_size: skipped, and
+ *              RPTQ_ERR_BAD_SLOT is recorded in the device's status word. No slot may be named twice in a call
+ *              (what such a slot then holds is not specified; no other slot is affected)
+ * Every other slot of the pool keeps its codes. Rows that are 16-byte aligned (base, row distance and head) are read 16 bytes at a
+ * time, others element by element.
+ */
+int rptq_kv_cache_write(const rptq_kv_cache_t* cache, const void* k, int64_t ldk, const void* v, int64_t ldv, int rows_type,
+                        const int64_t* slots, int n_tokens, void* k_pages, void* v_pages, int64_t n_pages, void* stream);
+
+/*
+ * Rows of the cache read back: row i receives s_c (q - z_c) of slot slots[i] (fp32, rounded to rows_type), original channel order; with
+ * RPTQ_ROWS_CODES the packed code rows of LK / LV, pads 0, as rptq_attention, rptq_attention_kv and rptq_code_rowsums read them. A
+ * negative slot, or one past the pool (recorded as above), leaves its row as it is. A slot may be named any number of times.
+ */
+int rptq_kv_cache_read(const rptq_kv_cache_t* cache, const void* k_pages, const void* v_pages, int64_t n_pages, const int64_t* slots,
+                       int n_tokens, void* k, int64_t ldk, void* v, int64_t ldv, int rows_type, void* stream);
+
+/*
+ * One new token per sequence attends over the sequence's cached keys (its own among them, written before). For sequence i, query head hq
+ * (which reads cached head h = hq / (n_q_heads / n_heads)) and key j < seq_lens[i]:
+ *   S[j]  = qk_scale * sum_ch Q[ch] s^K[ch] (K_q[j][ch] - z^K[ch]),  P = softmax of S,  O[ch] = s^V[ch] (sum_j P[j] V_q[j][ch] - z^V[ch])
+ * K's zero points shift all scores of a row alike and are not formed.
+ *   q, out      dev [n_seq][ldq], [n_seq][ldo] of q_type (RPTQ_ROWS_F16 or RPTQ_ROWS_BF16), n_q_heads * d elements a row
+ *   page_table  dev int32 [n_seq][ld_table]: entry j is the pool's page of the sequence's keys j * page_size ..; the first
+ *               ceil(seq_lens[i] / page_size) entries of a row are read
+ *   seq_lens    dev int32 [n_seq], 0 .. table_width * page_size (values outside are clamped). Length 0 gives zeros
+ *   workspace   dev, rptq_attention_paged_workspace_bytes(cache, n_q_heads) bytes, 16-byte aligned; nothing needs to be in it, and
+ *               nothing is kept in it between calls. Calls that may overlap on the GPU need a workspace each
+ * An entry outside 0 .. n_pages - 1 records RPTQ_ERR_BAD_SLOT in the status word and its keys are left out. What the slots behind a
+ * sequence's last key hold does not matter. A query that is not finite gives NaN. n_seq, n_q_heads <= 65535,
+ * table_width * page_size < 2^31.
+ */
+int64_t rptq_attention_paged_workspace_bytes(const rptq_kv_cache_t* cache, int n_q_heads);
+int rptq_attention_paged(const rptq_kv_cache_t* cache, const void* q, int64_t ldq, int q_type, int n_q_heads, int n_seq,
+                         const void* k_pages, const void* v_pages, int64_t n_pages, const int32_t* page_table, int64_t ld_table, int table_width,
+                         const int32_t* seq_lens, float qk_scale, void* out, int64_t ldo, void* workspace, void* stream);
 
 const char* rptq_status_string(int status);
 int rptq_format_version(void);

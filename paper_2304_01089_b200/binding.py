@@ -15,8 +15,9 @@ import numpy as np
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "librptq.so")
 
-OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_NOT_BIJECTION, ERR_CUDA, ERR_DEVICE_TIMEOUT, ERR_ALLOC = 0, -1, -2, -3, -4, -5, -6
+OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_NOT_BIJECTION, ERR_CUDA, ERR_DEVICE_TIMEOUT, ERR_ALLOC, ERR_BAD_SLOT = 0, -1, -2, -3, -4, -5, -6, -7
 OUT_F32, OUT_F16, OUT_CODES = 0, 1, 2
+ROWS_F32, ROWS_F16, ROWS_CODES, ROWS_BF16 = 0, 1, 2, 3
 ACT_NONE, ACT_RELU = 0, 1
 NOALLOC_MAX_N = 65536
 ORDER_CONTIGUOUS, ORDER_INTERLEAVED = 0, 1
@@ -28,7 +29,8 @@ EXPORTS = (
     "rptq_format_version", "rptq_layout_padded_index", "rptq_weight_codes_bytes", "rptq_cluster_gemm_noalloc",
     "rptq_selftest_ln_timeout", "rptq_dequant_gemm", "rptq_ln_channel_minmax", "rptq_kmeans", "rptq_kmeans_workspace_bytes",
     "rptq_probe_int8_peak", "rptq_weight_pack_clustered", "rptq_code_rowsums", "rptq_cluster_gemm_clustered",
-    "rptq_attention", "rptq_attention_kv",
+    "rptq_attention", "rptq_attention_kv", "rptq_kv_cache_create", "rptq_kv_cache_query", "rptq_kv_cache_destroy",
+    "rptq_kv_cache_write", "rptq_kv_cache_read", "rptq_attention_paged", "rptq_attention_paged_workspace_bytes",
 )
 
 
@@ -72,11 +74,19 @@ def _load(path: str = LIB_PATH) -> C.CDLL:
     lib.rptq_status_string.restype = C.c_char_p
     lib.rptq_attention.argtypes = [vp, vp, vp, i32, vp, i32, vp, vp, i32, i32, f32, i32, f32, i32, vp, i64, vp, vp]
     lib.rptq_attention_kv.argtypes = [vp, vp, i32, vp, i64, i32, vp, vp, i32, i32, f32, i32, vp, i64, vp]
+    lib.rptq_kv_cache_create.argtypes = [C.POINTER(vp), vp, vp, i32, i32]
+    lib.rptq_kv_cache_query.argtypes = [vp, C.POINTER(i64), C.POINTER(i64)]
+    lib.rptq_kv_cache_destroy.argtypes = [vp]
+    lib.rptq_kv_cache_write.argtypes = [vp, vp, i64, vp, i64, i32, vp, i32, vp, vp, i64, vp]
+    lib.rptq_kv_cache_read.argtypes = [vp, vp, vp, i64, vp, i32, vp, i64, vp, i64, i32, vp]
+    lib.rptq_attention_paged_workspace_bytes.argtypes = [vp, i32]
+    lib.rptq_attention_paged.argtypes = [vp, vp, i64, i32, i32, i32, vp, vp, i64, vp, i64, i32, vp, f32, vp, i64, vp, vp]
     for name in EXPORTS:
-        if name not in ("rptq_status_string", "rptq_weight_codes_bytes", "rptq_kmeans_workspace_bytes"):
+        if name not in ("rptq_status_string", "rptq_weight_codes_bytes", "rptq_kmeans_workspace_bytes", "rptq_attention_paged_workspace_bytes"):
             getattr(lib, name).restype = i32
     lib.rptq_weight_codes_bytes.restype = i64
     lib.rptq_kmeans_workspace_bytes.restype = i64
+    lib.rptq_attention_paged_workspace_bytes.restype = i64
     return lib
 
 
@@ -241,6 +251,144 @@ def attention_kv(LK: Layout, LV: Layout, n_heads: int, q, k_codes, v_codes, out,
     _check(_lib.rptq_attention_kv(LK.handle, LV.handle, int(n_heads), _dev_ptr(q), int(q.stride(0)), Tq, _dev_ptr(k_codes),
                                   _dev_ptr(v_codes), Tk, int(n_seq), C.c_float(qk_scale), 1 if causal else 0,
                                   _dev_ptr(out), int(out.stride(0)), _stream_ptr(stream)), "rptq_attention_kv")
+
+
+_rows_types = None               # torch dtype -> RPTQ_ROWS_*
+
+
+def _rows(t, what: str, n_rows: int, n_cols: int):
+    """(pointer, elements between rows, RPTQ_ROWS_* type) of a 2-D CUDA tensor whose rows are contiguous."""
+    global _rows_types
+    if _rows_types is None:
+        import torch
+        _rows_types = {torch.float32: ROWS_F32, torch.float16: ROWS_F16, torch.uint8: ROWS_CODES, torch.bfloat16: ROWS_BF16}
+    kind = _rows_types.get(t.dtype)
+    if kind is None:
+        raise ValueError(f"{what}: rows of {t.dtype} are not supported")
+    if not t.is_cuda or t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise ValueError(f"{what}: expected a 2-D CUDA tensor with contiguous rows")
+    if t.shape[0] < n_rows or t.shape[1] < n_cols:
+        raise ValueError(f"{what}: expected at least {n_rows} rows of {n_cols}, got {tuple(t.shape)}")
+    return t.data_ptr(), int(t.stride(0)) if t.shape[0] > 1 else int(t.shape[1]), kind
+
+
+def _ints(t, dtype_name: str, what: str, dim: int):
+    if not t.is_cuda or str(t.dtype) != "torch." + dtype_name or t.dim() != dim or (t.shape[-1] > 1 and t.stride(-1) != 1):
+        raise ValueError(f"{what}: expected a {dim}-D CUDA tensor of {dtype_name}")
+    return t.data_ptr()
+
+
+class KvCache:
+    """rptq_kv_cache_create / _query / _destroy: what a paged key / value cache looks like. It owns no pages: a pool is a
+    contiguous uint8 CUDA tensor of n_pages rows of k_page_bytes (v_page_bytes)."""
+
+    def __init__(self, layout_k: Layout, layout_v: Layout, n_heads: int, page_size: int):
+        import torch
+        h = C.c_void_p()
+        _check(_lib.rptq_kv_cache_create(C.byref(h), layout_k.handle, layout_v.handle, int(n_heads), int(page_size)), "rptq_kv_cache_create")
+        self._h = h
+        self.C, self.n_heads, self.page_size = layout_k.C, int(n_heads), int(page_size)
+        self.head_dim = self.C // self.n_heads
+        self.device = torch.cuda.current_device() if torch.cuda.is_available() else -1
+        self.k_row_bytes, self.v_row_bytes = layout_k.row_bytes, layout_v.row_bytes
+        kb, vb = C.c_int64(), C.c_int64()
+        _check(_lib.rptq_kv_cache_query(self._h, C.byref(kb), C.byref(vb)), "rptq_kv_cache_query")
+        self.k_page_bytes, self.v_page_bytes = int(kb.value), int(vb.value)
+
+    @property
+    def handle(self) -> C.c_void_p:
+        if self._h is None:
+            raise ValueError("cache was destroyed")
+        return self._h
+
+    def pools(self, k_pages, v_pages) -> int:
+        """Pages in the two pools."""
+        for t, b in ((k_pages, self.k_page_bytes), (v_pages, self.v_page_bytes)):
+            if str(t.dtype) != "torch.uint8" or t.dim() != 2 or t.shape[1] != b:
+                raise ValueError(f"a pool is uint8 [n_pages][{b}], got {t.dtype} {tuple(t.shape)}")
+        if k_pages.shape[0] != v_pages.shape[0]:
+            raise ValueError("the pools of keys and values have different numbers of pages")
+        return int(k_pages.shape[0])
+
+    def destroy(self) -> None:
+        if getattr(self, "_h", None) is not None:
+            _lib.rptq_kv_cache_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+
+def _on_device(cache: KvCache, *tensors) -> None:
+    if any(t.get_device() != cache.device for t in tensors):
+        raise ValueError("a tensor of the call is on another device than the cache's")
+
+
+def _cache_rows(cache: KvCache, k, v, n: int):
+    codes = str(k.dtype) == "torch.uint8"
+    pk, ldk, kind = _rows(k, "k", n, cache.k_row_bytes if codes else cache.C)
+    pv, ldv, kind_v = _rows(v, "v", n, cache.v_row_bytes if codes else cache.C)
+    if kind != kind_v:
+        raise ValueError("k and v have different types")
+    return pk, ldk, pv, ldv, kind
+
+
+def kv_cache_write(cache: KvCache, k, v, slots, k_pages, v_pages, stream=None) -> None:
+    """rptq_kv_cache_write: k, v [n][>= C] of fp16, bf16 or fp32 (original channel order; rows may lie apart, as in a slice of a fused
+    projection's output), or uint8 code rows [n][>= row_bytes] of the layouts; slots int64 [n] (negative: skipped);
+    k_pages, v_pages uint8 [n_pages][page bytes]. CUDA tensors."""
+    n, n_pages = int(slots.shape[0]), cache.pools(k_pages, v_pages)
+    pk, ldk, pv, ldv, kind = _cache_rows(cache, k, v, n)
+    _on_device(cache, k, v, slots, k_pages, v_pages)
+    _check(_lib.rptq_kv_cache_write(cache.handle, pk, ldk, pv, ldv, kind, _ints(slots, "int64", "slots", 1), n, _dev_ptr(k_pages),
+                                    _dev_ptr(v_pages), n_pages, _stream_ptr(stream)), "rptq_kv_cache_write")
+
+
+def kv_cache_read(cache: KvCache, k_pages, v_pages, slots, k_out, v_out, stream=None) -> None:
+    """rptq_kv_cache_read: row i of k_out, v_out (fp16, bf16, fp32 [n][>= C], or uint8 code rows [n][>= row_bytes]) receives slot
+    slots[i]; rows of negative slots stay as they are."""
+    n, n_pages = int(slots.shape[0]), cache.pools(k_pages, v_pages)
+    pk, ldk, pv, ldv, kind = _cache_rows(cache, k_out, v_out, n)
+    _on_device(cache, k_out, v_out, slots, k_pages, v_pages)
+    _check(_lib.rptq_kv_cache_read(cache.handle, _dev_ptr(k_pages), _dev_ptr(v_pages), n_pages, _ints(slots, "int64", "slots", 1), n,
+                                   pk, ldk, pv, ldv, kind, _stream_ptr(stream)), "rptq_kv_cache_read")
+
+
+def attention_paged_workspace_bytes(cache: KvCache, n_q_heads: Optional[int] = None) -> int:
+    n = int(_lib.rptq_attention_paged_workspace_bytes(cache.handle, cache.n_heads if n_q_heads is None else int(n_q_heads)))
+    if n < 0:
+        raise RptqError(n, "rptq_attention_paged_workspace_bytes")
+    return n
+
+
+def attention_paged(cache: KvCache, q, k_pages, v_pages, page_table, seq_lens, out, qk_scale: float, n_q_heads: Optional[int] = None,
+                    workspace=None, stream=None) -> None:
+    """rptq_attention_paged: q, out fp16 or bf16 [n_seq][>= n_q_heads * d], page_table int32 [n_seq][pages], seq_lens int32 [n_seq]; CUDA
+    tensors. n_q_heads: a multiple of the cache's heads (default: as many). workspace: uint8 of
+    attention_paged_workspace_bytes(cache, n_q_heads) bytes, allocated by the call if None."""
+    n_q_heads = cache.n_heads if n_q_heads is None else int(n_q_heads)
+    n_seq, n_pages, cols = int(seq_lens.shape[0]), cache.pools(k_pages, v_pages), n_q_heads * cache.head_dim
+    pq, ldq, kind = _rows(q, "q", n_seq, cols)
+    po, ldo, kind_o = _rows(out, "out", n_seq, cols)
+    if kind != kind_o:
+        raise ValueError("q and out have different types")
+    table, lens = _ints(page_table, "int32", "page_table", 2), _ints(seq_lens, "int32", "seq_lens", 1)
+    if page_table.shape[0] < n_seq:
+        raise ValueError("page_table has fewer rows than there are sequences")
+    need = attention_paged_workspace_bytes(cache, n_q_heads)
+    if workspace is None:
+        import torch
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    if workspace.numel() * workspace.element_size() < need:
+        raise ValueError(f"workspace: {need} bytes are needed")
+    _on_device(cache, q, out, page_table, seq_lens, k_pages, v_pages, workspace)
+    width = int(page_table.shape[1])
+    ld_table = int(page_table.stride(0)) if page_table.shape[0] > 1 else width
+    _check(_lib.rptq_attention_paged(cache.handle, pq, ldq, kind, n_q_heads, n_seq, _dev_ptr(k_pages), _dev_ptr(v_pages), n_pages, table, ld_table,
+                                     width, lens, C.c_float(qk_scale), po, ldo, _dev_ptr(workspace), _stream_ptr(stream)), "rptq_attention_paged")
 
 
 def weight_pack(layout_in: Layout, W: np.ndarray, out_perm=None, n_pad: Optional[int] = None):

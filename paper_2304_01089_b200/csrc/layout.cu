@@ -146,6 +146,7 @@ const char* rptq_status_string(int status)
         case RPTQ_ERR_CUDA: return "CUDA call failed";
         case RPTQ_ERR_DEVICE_TIMEOUT: return "bounded wait inside a kernel ran out";
         case RPTQ_ERR_ALLOC: return "allocation failed";
+        case RPTQ_ERR_BAD_SLOT: return "slot or page outside its pool";
         default: return "unknown status";
     }
 }
