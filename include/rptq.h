@@ -406,7 +406,7 @@ int rptq_attention_kv(const rptq_layout_t* LK, const rptq_layout_t* LV, int n_he
  *   LK, LV     the layouts of the attention sites, as for rptq_attention_kv (3, 4 or 8 bits each); their cluster parameters are
  *              copied. Only which channel has which (s_c, z_c) matters here: any reorder index and unit order will do
  *   n_heads    heads of the cache; head h owns the channels h * d .. (h + 1) * d - 1, d = C / n_heads <= 256
- *   page_size  keys per page, a multiple of 16, at most 65536
+ *   page_size  keys per page, a multiple of 16, at most 65536; a page of either tensor is at most 2^31 - 1 bytes
  * A pool is n_pages pages of k_page_bytes (v_page_bytes) bytes, one after the other, 16-byte aligned. Slot s is key s % page_size of page
  * s / page_size. The bytes inside a page are the library's choice (format version 2): channels in their own order, a head's rounded up
  * to a multiple of 32, so a page takes page_size * n_heads * roundup32(d) * bits / 8 bytes.

@@ -253,28 +253,26 @@ def attention_kv(LK: Layout, LV: Layout, n_heads: int, q, k_codes, v_codes, out,
                                   _dev_ptr(out), int(out.stride(0)), _stream_ptr(stream)), "rptq_attention_kv")
 
 
-_rows_types = None               # torch dtype -> RPTQ_ROWS_*
+_torch = None                    # set with the first KvCache
+_rows_types = {}                 # torch dtype -> RPTQ_ROWS_*
 
 
-def _rows(t, what: str, n_rows: int, n_cols: int):
+def _rows(t, what: str, device: int, n_rows: int, n_cols: int):
     """(pointer, elements between rows, RPTQ_ROWS_* type) of a 2-D CUDA tensor whose rows are contiguous."""
-    global _rows_types
-    if _rows_types is None:
-        import torch
-        _rows_types = {torch.float32: ROWS_F32, torch.float16: ROWS_F16, torch.uint8: ROWS_CODES, torch.bfloat16: ROWS_BF16}
-    kind = _rows_types.get(t.dtype)
+    kind, shape, stride = _rows_types.get(t.dtype), t.shape, t.stride()
     if kind is None:
         raise ValueError(f"{what}: rows of {t.dtype} are not supported")
-    if not t.is_cuda or t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
-        raise ValueError(f"{what}: expected a 2-D CUDA tensor with contiguous rows")
-    if t.shape[0] < n_rows or t.shape[1] < n_cols:
-        raise ValueError(f"{what}: expected at least {n_rows} rows of {n_cols}, got {tuple(t.shape)}")
-    return t.data_ptr(), int(t.stride(0)) if t.shape[0] > 1 else int(t.shape[1]), kind
+    if t.get_device() != device or len(shape) != 2 or (stride[1] != 1 and shape[1] > 1):
+        raise ValueError(f"{what}: expected a 2-D tensor with contiguous rows on the cache's device")
+    if shape[0] < n_rows or shape[1] < n_cols:
+        raise ValueError(f"{what}: expected at least {n_rows} rows of {n_cols}, got {tuple(shape)}")
+    return t.data_ptr(), stride[0] if shape[0] > 1 else shape[1], kind
 
 
-def _ints(t, dtype_name: str, what: str, dim: int):
-    if not t.is_cuda or str(t.dtype) != "torch." + dtype_name or t.dim() != dim or (t.shape[-1] > 1 and t.stride(-1) != 1):
-        raise ValueError(f"{what}: expected a {dim}-D CUDA tensor of {dtype_name}")
+def _ints(t, what: str, device: int, dtype, dim: int):
+    shape = t.shape
+    if t.dtype is not dtype or t.get_device() != device or len(shape) != dim or (shape[-1] > 1 and t.stride()[-1] != 1):
+        raise ValueError(f"{what}: expected a {dim}-D tensor of {dtype} on the cache's device")
     return t.data_ptr()
 
 
@@ -283,17 +281,22 @@ class KvCache:
     contiguous uint8 CUDA tensor of n_pages rows of k_page_bytes (v_page_bytes)."""
 
     def __init__(self, layout_k: Layout, layout_v: Layout, n_heads: int, page_size: int):
-        import torch
+        global _torch
+        if _torch is None:
+            import torch
+            _rows_types.update({torch.float32: ROWS_F32, torch.float16: ROWS_F16, torch.uint8: ROWS_CODES, torch.bfloat16: ROWS_BF16})
+            _torch = torch
         h = C.c_void_p()
         _check(_lib.rptq_kv_cache_create(C.byref(h), layout_k.handle, layout_v.handle, int(n_heads), int(page_size)), "rptq_kv_cache_create")
         self._h = h
         self.C, self.n_heads, self.page_size = layout_k.C, int(n_heads), int(page_size)
         self.head_dim = self.C // self.n_heads
-        self.device = torch.cuda.current_device() if torch.cuda.is_available() else -1
+        self.device = _torch.cuda.current_device() if _torch.cuda.is_available() else -1
         self.k_row_bytes, self.v_row_bytes = layout_k.row_bytes, layout_v.row_bytes
         kb, vb = C.c_int64(), C.c_int64()
         _check(_lib.rptq_kv_cache_query(self._h, C.byref(kb), C.byref(vb)), "rptq_kv_cache_query")
         self.k_page_bytes, self.v_page_bytes = int(kb.value), int(vb.value)
+        self._workspace = {}                               # query heads -> bytes
 
     @property
     def handle(self) -> C.c_void_p:
@@ -301,14 +304,15 @@ class KvCache:
             raise ValueError("cache was destroyed")
         return self._h
 
-    def pools(self, k_pages, v_pages) -> int:
-        """Pages in the two pools."""
+    def pools(self, k_pages, v_pages):
+        """(pointer, pointer, pages) of the two pools."""
         for t, b in ((k_pages, self.k_page_bytes), (v_pages, self.v_page_bytes)):
-            if str(t.dtype) != "torch.uint8" or t.dim() != 2 or t.shape[1] != b:
-                raise ValueError(f"a pool is uint8 [n_pages][{b}], got {t.dtype} {tuple(t.shape)}")
+            shape = t.shape
+            if t.dtype is not _torch.uint8 or len(shape) != 2 or shape[1] != b or not t.is_contiguous() or t.get_device() != self.device:
+                raise ValueError(f"a pool is a contiguous uint8 [n_pages][{b}] on the cache's device, got {t.dtype} {tuple(shape)}")
         if k_pages.shape[0] != v_pages.shape[0]:
             raise ValueError("the pools of keys and values have different numbers of pages")
-        return int(k_pages.shape[0])
+        return k_pages.data_ptr(), v_pages.data_ptr(), k_pages.shape[0]
 
     def destroy(self) -> None:
         if getattr(self, "_h", None) is not None:
@@ -322,15 +326,10 @@ class KvCache:
             pass
 
 
-def _on_device(cache: KvCache, *tensors) -> None:
-    if any(t.get_device() != cache.device for t in tensors):
-        raise ValueError("a tensor of the call is on another device than the cache's")
-
-
 def _cache_rows(cache: KvCache, k, v, n: int):
-    codes = str(k.dtype) == "torch.uint8"
-    pk, ldk, kind = _rows(k, "k", n, cache.k_row_bytes if codes else cache.C)
-    pv, ldv, kind_v = _rows(v, "v", n, cache.v_row_bytes if codes else cache.C)
+    codes = k.dtype is _torch.uint8
+    pk, ldk, kind = _rows(k, "k", cache.device, n, cache.k_row_bytes if codes else cache.C)
+    pv, ldv, kind_v = _rows(v, "v", cache.device, n, cache.v_row_bytes if codes else cache.C)
     if kind != kind_v:
         raise ValueError("k and v have different types")
     return pk, ldk, pv, ldv, kind
@@ -340,55 +339,55 @@ def kv_cache_write(cache: KvCache, k, v, slots, k_pages, v_pages, stream=None) -
     """rptq_kv_cache_write: k, v [n][>= C] of fp16, bf16 or fp32 (original channel order; rows may lie apart, as in a slice of a fused
     projection's output), or uint8 code rows [n][>= row_bytes] of the layouts; slots int64 [n] (negative: skipped);
     k_pages, v_pages uint8 [n_pages][page bytes]. CUDA tensors."""
-    n, n_pages = int(slots.shape[0]), cache.pools(k_pages, v_pages)
+    at, n = _ints(slots, "slots", cache.device, _torch.int64, 1), slots.shape[0]
+    kp, vp, n_pages = cache.pools(k_pages, v_pages)
     pk, ldk, pv, ldv, kind = _cache_rows(cache, k, v, n)
-    _on_device(cache, k, v, slots, k_pages, v_pages)
-    _check(_lib.rptq_kv_cache_write(cache.handle, pk, ldk, pv, ldv, kind, _ints(slots, "int64", "slots", 1), n, _dev_ptr(k_pages),
-                                    _dev_ptr(v_pages), n_pages, _stream_ptr(stream)), "rptq_kv_cache_write")
+    _check(_lib.rptq_kv_cache_write(cache.handle, pk, ldk, pv, ldv, kind, at, n, kp, vp, n_pages, _stream_ptr(stream)), "rptq_kv_cache_write")
 
 
 def kv_cache_read(cache: KvCache, k_pages, v_pages, slots, k_out, v_out, stream=None) -> None:
     """rptq_kv_cache_read: row i of k_out, v_out (fp16, bf16, fp32 [n][>= C], or uint8 code rows [n][>= row_bytes]) receives slot
     slots[i]; rows of negative slots stay as they are."""
-    n, n_pages = int(slots.shape[0]), cache.pools(k_pages, v_pages)
+    at, n = _ints(slots, "slots", cache.device, _torch.int64, 1), slots.shape[0]
+    kp, vp, n_pages = cache.pools(k_pages, v_pages)
     pk, ldk, pv, ldv, kind = _cache_rows(cache, k_out, v_out, n)
-    _on_device(cache, k_out, v_out, slots, k_pages, v_pages)
-    _check(_lib.rptq_kv_cache_read(cache.handle, _dev_ptr(k_pages), _dev_ptr(v_pages), n_pages, _ints(slots, "int64", "slots", 1), n,
-                                   pk, ldk, pv, ldv, kind, _stream_ptr(stream)), "rptq_kv_cache_read")
+    _check(_lib.rptq_kv_cache_read(cache.handle, kp, vp, n_pages, at, n, pk, ldk, pv, ldv, kind, _stream_ptr(stream)), "rptq_kv_cache_read")
 
 
 def attention_paged_workspace_bytes(cache: KvCache, n_q_heads: Optional[int] = None) -> int:
-    n = int(_lib.rptq_attention_paged_workspace_bytes(cache.handle, cache.n_heads if n_q_heads is None else int(n_q_heads)))
-    if n < 0:
-        raise RptqError(n, "rptq_attention_paged_workspace_bytes")
+    n_q_heads = cache.n_heads if n_q_heads is None else int(n_q_heads)
+    n = cache._workspace.get(n_q_heads)
+    if n is None:
+        n = int(_lib.rptq_attention_paged_workspace_bytes(cache.handle, n_q_heads))
+        if n < 0:
+            raise RptqError(n, "rptq_attention_paged_workspace_bytes")
+        cache._workspace[n_q_heads] = n
     return n
 
 
 def attention_paged(cache: KvCache, q, k_pages, v_pages, page_table, seq_lens, out, qk_scale: float, n_q_heads: Optional[int] = None,
                     workspace=None, stream=None) -> None:
     """rptq_attention_paged: q, out fp16 or bf16 [n_seq][>= n_q_heads * d], page_table int32 [n_seq][pages], seq_lens int32 [n_seq]; CUDA
-    tensors. n_q_heads: a multiple of the cache's heads (default: as many). workspace: uint8 of
+    tensors. n_q_heads: a multiple of the cache's heads (default: as many). workspace: a contiguous tensor of at least
     attention_paged_workspace_bytes(cache, n_q_heads) bytes, allocated by the call if None."""
-    n_q_heads = cache.n_heads if n_q_heads is None else int(n_q_heads)
-    n_seq, n_pages, cols = int(seq_lens.shape[0]), cache.pools(k_pages, v_pages), n_q_heads * cache.head_dim
-    pq, ldq, kind = _rows(q, "q", n_seq, cols)
-    po, ldo, kind_o = _rows(out, "out", n_seq, cols)
+    n_q_heads, device = cache.n_heads if n_q_heads is None else int(n_q_heads), cache.device
+    lens, n_seq = _ints(seq_lens, "seq_lens", device, _torch.int32, 1), seq_lens.shape[0]
+    kp, vp, n_pages = cache.pools(k_pages, v_pages)
+    cols = n_q_heads * cache.head_dim
+    pq, ldq, kind = _rows(q, "q", device, n_seq, cols)
+    po, ldo, kind_o = _rows(out, "out", device, n_seq, cols)
     if kind != kind_o:
         raise ValueError("q and out have different types")
-    table, lens = _ints(page_table, "int32", "page_table", 2), _ints(seq_lens, "int32", "seq_lens", 1)
-    if page_table.shape[0] < n_seq:
+    table, (n_rows, width) = _ints(page_table, "page_table", device, _torch.int32, 2), page_table.shape
+    if n_rows < n_seq:
         raise ValueError("page_table has fewer rows than there are sequences")
     need = attention_paged_workspace_bytes(cache, n_q_heads)
     if workspace is None:
-        import torch
-        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-    if workspace.numel() * workspace.element_size() < need:
-        raise ValueError(f"workspace: {need} bytes are needed")
-    _on_device(cache, q, out, page_table, seq_lens, k_pages, v_pages, workspace)
-    width = int(page_table.shape[1])
-    ld_table = int(page_table.stride(0)) if page_table.shape[0] > 1 else width
-    _check(_lib.rptq_attention_paged(cache.handle, pq, ldq, kind, n_q_heads, n_seq, _dev_ptr(k_pages), _dev_ptr(v_pages), n_pages, table, ld_table,
-                                     width, lens, C.c_float(qk_scale), po, ldo, _dev_ptr(workspace), _stream_ptr(stream)), "rptq_attention_paged")
+        workspace = _torch.empty(need, dtype=_torch.uint8, device=q.device)
+    if workspace.nbytes < need or not workspace.is_contiguous() or workspace.get_device() != device:
+        raise ValueError(f"workspace: {need} contiguous bytes on the cache's device are needed")
+    _check(_lib.rptq_attention_paged(cache.handle, pq, ldq, kind, n_q_heads, n_seq, kp, vp, n_pages, table, page_table.stride(0) if n_rows > 1 else width,
+                                     width, lens, qk_scale, po, ldo, workspace.data_ptr(), _stream_ptr(stream)), "rptq_attention_paged")
 
 
 def weight_pack(layout_in: Layout, W: np.ndarray, out_perm=None, n_pad: Optional[int] = None):

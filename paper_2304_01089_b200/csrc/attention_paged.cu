@@ -1,4 +1,8 @@
 // rptq_attention_paged: argument checks, the choice of the kernel's instance, and the launches. The kernel: attention_paged.cuh.
+#include <atomic>
+#include <chrono>
+#include <climits>
+
 #include "attention_paged.cuh"
 #include "attention_paged_launch.h"
 
@@ -17,16 +21,18 @@ static Plan plan_of(const rptq_kv_cache_t* c, int G)
     x.un = c->nu <= 4 ? 4 : 8;
     x.nq = G <= 2 ? 2 : G <= 4 || x.un == 8 ? 4 : 8;
     x.chunks = (G + x.nq - 1) / x.nq;
-    x.smem = WARPS * (STAGES * stage_bytes((int)c->k.slab_bytes, (int)c->v.slab_bytes) + scratch_bytes(x.un, x.nq));
+    x.smem = WARPS * (STAGES * stage_bytes(c->k.bits, c->v.bits, c->nu) + scratch_bytes(x.un, x.nq));
     const int by_smem = (SMEM_MAX + 1024) / (x.smem + 1024), by_regs = x.un == 4 && x.nq <= 4 ? 4 : 3;
     x.blocks_per_sm = by_smem < by_regs ? by_smem : by_regs;
     return x;
 }
 
-template <int NQ>
-static int launch_join(const Params& p, int grid, cudaStream_t st)
+// A mark that no other call of the process has, in the upper 48 bits; where the marks begin is drawn from the clock, so that what an earlier
+// process left in the memory is not taken for one of them either.
+static unsigned long long new_mark()
 {
-    return launch_kernel(join_kernel<NQ>, dim3((unsigned)(grid * WARPS - 1)), THREADS, 0, 0, st, p, (int64_t)grid * WARPS);
+    static std::atomic<unsigned long long> next{(unsigned long long)std::chrono::steady_clock::now().time_since_epoch().count() * 0x9E3779B97F4A7C15ull};
+    return next.fetch_add(1ull << 16, std::memory_order_relaxed) & ~0xFFFFull;
 }
 
 }  // namespace attn_paged
@@ -42,7 +48,7 @@ int64_t rptq_attention_paged_workspace_bytes(const rptq_kv_cache_t* cache, int n
     const int n_sm = cache->device < 0 ? 0 : sm_count(cache->device);
     if (n_sm == 0) return RPTQ_ERR_CUDA;
     const Plan x = plan_of(cache, n_q_heads / cache->H);
-    return (int64_t)n_sm * x.blocks_per_sm * WARPS * 2 * part_floats(x.nq, cache->nu) * 4;
+    return (int64_t)n_sm * x.blocks_per_sm * WARPS * (8 + 2 * 4 * part_floats(x.nq, cache->nu));
 }
 
 int rptq_attention_paged(const rptq_kv_cache_t* cache, const void* q, int64_t ldq, int q_type, int n_q_heads, int n_seq,
@@ -70,17 +76,20 @@ int rptq_attention_paged(const rptq_kv_cache_t* cache, const void* q, int64_t ld
 
     Params p{};
     p.k = static_cast<const uint8_t*>(k_pages); p.v = static_cast<const uint8_t*>(v_pages);
-    p.k_slab = (int)cache->k.slab_bytes; p.v_slab = (int)cache->v.slab_bytes; p.k_page = cache->k.page_bytes; p.v_page = cache->v.page_bytes; p.n_pages = n_pages;
+    p.k_page = (uint32_t)cache->k.page_bytes; p.v_page = (uint32_t)cache->v.page_bytes;
+    p.n_pages = (uint32_t)(n_pages < INT_MAX ? n_pages : INT_MAX);          // (a page number is an int32)
     p.val_k = cache->k.value; p.val_v = cache->v.value;
     p.q = q; p.ldq = ldq; p.out = out; p.ldo = ldo; p.bf16 = q_type == RPTQ_ROWS_BF16;
     p.vector_out = aligned16(out) && ldo % 8 == 0 && cache->d % 8 == 0;
-    p.table = page_table; p.ld_table = ld_table; p.width = table_width; p.lens = seq_lens;
+    p.table = page_table; p.ld_table = ld_table; p.lens = seq_lens;
     p.n_seq = n_seq; p.H = cache->H; p.G = n_q_heads / cache->H; p.d = cache->d; p.nu = cache->nu; p.P = cache->P;
     p.max_len = table_width * cache->P;
     const Plan x = plan_of(cache, p.G);
     p.chunks = x.chunks;
     p.scale_log2e = qk_scale * 1.4426950408889634f;
-    p.parts = static_cast<float*>(workspace);
+    p.arrived = static_cast<unsigned long long*>(workspace);
+    p.call = new_mark();
+    p.parts = reinterpret_cast<float*>(p.arrived + (int64_t)n_sm * x.blocks_per_sm * WARPS);
     p.status = device_status_word();
 
     // what the longest sequences could need, in warps; a grid that fills the GPU is the most
@@ -91,9 +100,7 @@ int rptq_attention_paged(const rptq_kv_cache_t* cache, const void* q, int64_t ld
     Launch l{};
     l.bits_v = cache->v.bits; l.un = x.un; l.nq = x.nq; l.smem = x.smem; l.dev = dev; l.stream = static_cast<cudaStream_t>(stream);
     l.grid = (int)(warps < most ? (warps < 1 ? 1 : warps) : most);
-    const int rc = cache->k.bits == 3 ? launch_keys3(p, l) : cache->k.bits == 4 ? launch_keys4(p, l) : launch_keys8(p, l);
-    if (rc != RPTQ_OK || p.whole) return rc;
-    return x.nq == 2 ? launch_join<2>(p, l.grid, l.stream) : x.nq == 4 ? launch_join<4>(p, l.grid, l.stream) : launch_join<8>(p, l.grid, l.stream);
+    return cache->k.bits == 3 ? launch_keys3(p, l) : cache->k.bits == 4 ? launch_keys4(p, l) : launch_keys8(p, l);
 }
 
 }  // extern "C"

@@ -299,6 +299,8 @@ int rptq_kv_cache_create(rptq_kv_cache_t** out, const rptq_layout_t* LK, const r
     if (!LK || !LV || n_heads < 1 || page_size < 1) return RPTQ_ERR_INVALID_ARG;
     if (LK->C != LV->C || LK->C % n_heads || LK->device != LV->device) return RPTQ_ERR_INVALID_ARG;
     if (LK->C / n_heads > 32 * MAX_UNITS || page_size % SLAB || page_size > 65536) return RPTQ_ERR_UNSUPPORTED;
+    const int bits = LK->bits > LV->bits ? LK->bits : LV->bits;             // offsets inside a page are 32 bits
+    if ((int64_t)page_size * n_heads * ((LK->C / n_heads + 31) / 32) * 4 * bits > INT_MAX) return RPTQ_ERR_UNSUPPORTED;
     int dev = -1;
     if (LK->device >= 0 && (cudaGetDevice(&dev) != cudaSuccess || dev != LK->device)) return RPTQ_ERR_INVALID_ARG;
     rptq_kv_cache_t* c = new (std::nothrow) rptq_kv_cache();
