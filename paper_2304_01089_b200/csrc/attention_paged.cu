@@ -1,5 +1,4 @@
 // rptq_attention_paged: argument checks, the choice of the kernel's instance, and the launches. The kernel: attention_paged.cuh.
-#include <atomic>
 #include <chrono>
 #include <climits>
 
@@ -10,29 +9,29 @@ namespace rptq {
 namespace attn_paged {
 
 constexpr int MAX_KEYS = 1 << 30;              // per sequence
-constexpr int MIN_TILES = 4;                   // least share of a warp
+constexpr int MIN_SHARE = PAIR_COST + 4;       // least share of a group
 constexpr int WHOLE_TILES = 4;                 // pairs of at most so many tiles are not split
 
-// How a cache is worked on with this many query heads per cached head.
-struct Plan { int un, nq, chunks, smem, blocks_per_sm; };
+// How a cache is worked on with G query heads per cached head: the instance knows its sizes (`exact`), warps of a group, blocks per SM.
+struct Plan { bool exact; int un, warps, chunks, smem, blocks_per_sm; };
 static Plan plan_of(const rptq_kv_cache_t* c, int G)
 {
     Plan x{};
-    x.un = c->nu <= 4 ? 4 : 8;
-    x.nq = G <= 2 ? 2 : G <= 4 || x.un == 8 ? 4 : 8;
-    x.chunks = (G + x.nq - 1) / x.nq;
-    x.smem = WARPS * (STAGES * stage_bytes(c->k.bits, c->v.bits, c->nu) + scratch_bytes(x.un, x.nq));
-    const int by_smem = (SMEM_MAX + 1024) / (x.smem + 1024), by_regs = x.un == 4 && x.nq <= 4 ? 4 : 3;
-    x.blocks_per_sm = by_smem < by_regs ? by_smem : by_regs;
+    x.exact = c->k.bits == c->v.bits && (c->nu == 8 || (c->nu >= 2 && c->nu <= 4));
+    x.un = x.exact ? c->nu : c->nu <= 4 ? 4 : 8;
+    x.warps = G <= WARP_Q ? 1 : G <= 2 * WARP_Q ? 2 : 4;
+    x.chunks = (G + x.warps * WARP_Q - 1) / (x.warps * WARP_Q);
+    x.smem = WARPS / x.warps * STAGES * stage_bytes(c->k.bits, c->v.bits, c->nu) + WARPS * scratch_bytes(x.un);
+    const int by_smem = (SMEM_MAX + 1024) / (x.smem + 1024);
+    x.blocks_per_sm = by_smem < BLOCKS_PER_SM ? by_smem : BLOCKS_PER_SM;
     return x;
 }
 
-// A mark that no other call of the process has, in the upper 48 bits; where the marks begin is drawn from the clock, so that what an earlier
-// process left in the memory is not taken for one of them either.
-static unsigned long long new_mark()
+// In the upper 48 bits; drawn from the clock, so that what an earlier process left in the memory is not taken for this one's counts.
+static unsigned long long process_mark()
 {
-    static std::atomic<unsigned long long> next{(unsigned long long)std::chrono::steady_clock::now().time_since_epoch().count() * 0x9E3779B97F4A7C15ull};
-    return next.fetch_add(1ull << 16, std::memory_order_relaxed) & ~0xFFFFull;
+    static const unsigned long long mark = ((unsigned long long)std::chrono::steady_clock::now().time_since_epoch().count() * 0x9E3779B97F4A7C15ull) & ~0xFFFFull;
+    return mark;
 }
 
 }  // namespace attn_paged
@@ -48,7 +47,7 @@ int64_t rptq_attention_paged_workspace_bytes(const rptq_kv_cache_t* cache, int n
     const int n_sm = cache->device < 0 ? 0 : sm_count(cache->device);
     if (n_sm == 0) return RPTQ_ERR_CUDA;
     const Plan x = plan_of(cache, n_q_heads / cache->H);
-    return (int64_t)n_sm * x.blocks_per_sm * WARPS * (8 + 2 * 4 * part_floats(x.nq, cache->nu));
+    return (int64_t)n_sm * x.blocks_per_sm * WARPS * (8 + 2 * WARP_Q * 4 * part_pitch(cache->nu));
 }
 
 int rptq_attention_paged(const rptq_kv_cache_t* cache, const void* q, int64_t ldq, int q_type, int n_q_heads, int n_seq,
@@ -88,18 +87,20 @@ int rptq_attention_paged(const rptq_kv_cache_t* cache, const void* q, int64_t ld
     p.chunks = x.chunks;
     p.scale_log2e = qk_scale * 1.4426950408889634f;
     p.arrived = static_cast<unsigned long long*>(workspace);
-    p.call = new_mark();
-    p.parts = reinterpret_cast<float*>(p.arrived + (int64_t)n_sm * x.blocks_per_sm * WARPS);
+    p.mark = process_mark();
     p.status = device_status_word();
+    p.warps = x.warps;
+    const int64_t most = (int64_t)n_sm * x.blocks_per_sm;
+    p.parts = reinterpret_cast<float*>(p.arrived + most * WARPS);
 
-    // what the longest sequences could need, in warps; a grid that fills the GPU is the most
+    // what the longest sequences could need; a grid that fills the GPU is the most
     const int64_t max_tiles = (p.max_len + TILE - 1) / TILE, all_pairs = (int64_t)n_seq * p.H * p.chunks;
     p.whole = max_tiles <= WHOLE_TILES;
-    p.min_tiles = MIN_TILES;
-    const int64_t warps = p.whole ? all_pairs : (all_pairs * max_tiles + MIN_TILES - 1) / MIN_TILES, most = (int64_t)n_sm * x.blocks_per_sm;
+    p.min_share = MIN_SHARE;
+    const int64_t groups = p.whole ? all_pairs : (all_pairs * (max_tiles + PAIR_COST) + MIN_SHARE - 1) / MIN_SHARE;
     Launch l{};
-    l.bits_v = cache->v.bits; l.un = x.un; l.nq = x.nq; l.smem = x.smem; l.dev = dev; l.stream = static_cast<cudaStream_t>(stream);
-    l.grid = (int)(warps < most ? (warps < 1 ? 1 : warps) : most);
+    l.bits_v = cache->v.bits; l.un = x.un; l.smem = x.smem; l.dev = dev; l.stream = static_cast<cudaStream_t>(stream);
+    l.grid = (int)(groups < most ? (groups < 1 ? 1 : groups) : most);       // (every block's first group has a share before any has a second)
     return cache->k.bits == 3 ? launch_keys3(p, l) : cache->k.bits == 4 ? launch_keys4(p, l) : launch_keys8(p, l);
 }
 
