@@ -1,10 +1,18 @@
 // The paged key / value cache: handle, quantise-on-write and read-back.
+//
+// Writing reads 2 to 4 bytes and writes 3 to 8 bits an element, reading back the reverse: both are bound by memory. A warp takes 256 channels
+// (8 a lane: one 16-byte access of 16-bit rows, one word of 4-bit codes) of the tokens of a window, and keeps their parameters in
+// registers. Tokens whose slots follow one another inside a group of four keys (a prompt's, whatever key it starts at) are taken together: the
+// bytes of V that one token owns lie four apart, but four tokens' bytes of a word are 16 in a row (a 4 x 4 transposition in registers). One
+// token alone writes its bytes one by one.
+// LATER
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
 #include <climits>
 #include <cstring>
 #include <new>
+#include <type_traits>
 
 #include "kv_pages.cuh"
 #include "pack.cuh"
@@ -31,10 +39,13 @@ struct Side {
 struct Params {
     Side side[2];                  // K, V
     const int64_t* slots;
-    int n_tokens, H, d, nu, P, C;
+    int n_tokens, H, d, nu, P;
+    int window;                    // tokens a warp looks at, 1 .. 32
     int64_t n_slots;
     int* status;
 };
+
+__device__ __forceinline__ int64_t page_of(int64_t slot, int P) { return slot >> 31 ? slot / P : (int64_t)((uint32_t)slot / (uint32_t)P); }
 
 // A token's key in its page; false: the token is left alone.
 __device__ __forceinline__ bool find_slot(const Params& p, int token, int64_t& page, int& key)
@@ -45,7 +56,7 @@ __device__ __forceinline__ bool find_slot(const Params& p, int token, int64_t& p
         if (p.status) *p.status = RPTQ_ERR_BAD_SLOT;
         return false;
     }
-    page = slot / p.P;
+    page = page_of(slot, p.P);
     key = (int)(slot - page * p.P);
     return true;
 }
@@ -70,6 +81,263 @@ __device__ __forceinline__ uint32_t row_code(const uint8_t* row, int pos)
     return ((u[at] >> (sh + 3)) & 1u) | (((u[4 + at] >> (sh + 3)) & 1u) << 1) | (((u[8 + at] >> (sh + 3)) & 1u) << 2);
 }
 
+// ---------------------------------------------------------------- rows of values
+// The tokens of a warp's window that go together: lane l stands for token first + l. A token leads when it is the first of its call in a
+// group of four keys whose slots follow one another; `n` tokens from it on are its group.
+struct Window { int64_t slot; int n; uint32_t leaders; };
+__device__ __forceinline__ Window find_groups(const Params& p, int first)
+{
+    const int lane = threadIdx.x & 31, i = first + lane;
+    Window w{-1, 0, 0u};
+    bool leads = false;
+    if (lane < p.window && i < p.n_tokens) {
+        const int64_t s = p.slots[i];
+        if (s >= p.n_slots) {
+            if (p.status) *p.status = RPTQ_ERR_BAD_SLOT;
+        } else if (s >= 0) {
+            const int in_four = (int)(s & 3);
+            leads = in_four == 0 || i == 0 || p.slots[i - 1] != s - 1;
+            w.slot = s;
+            w.n = 1;
+            while (leads && in_four + w.n < 4 && i + w.n < p.n_tokens && p.slots[i + w.n] == s + w.n && s + w.n < p.n_slots) ++w.n;
+        }
+    }
+    w.leaders = __ballot_sync(0xffffffffu, leads);
+    return w;
+}
+// Eight channels of a head: the lane's place among all heads' groups of eight.
+struct Place { int h, u, w, ch, real; bool valid; };       // unit, group of the unit, first channel of the head, channels that exist
+__device__ __forceinline__ Place find_place(const Params& p, int group)
+{
+    Place x;
+    x.valid = group < p.H * p.nu * 4;
+    const int unit = group >> 2;
+    x.h = unit / p.nu;
+    x.u = unit - x.h * p.nu;
+    x.w = group & 3;
+    x.ch = 32 * x.u + 8 * x.w;
+    x.real = x.valid ? min(max(p.d - x.ch, 0), 8) : 0;
+    return x;
+}
+// byte e of word k -> byte k of word e
+__device__ __forceinline__ void transpose4(uint32_t (&w)[4])
+{
+    const uint32_t a = __byte_perm(w[0], w[1], 0x5140), b = __byte_perm(w[0], w[1], 0x7362);
+    const uint32_t c = __byte_perm(w[2], w[3], 0x5140), d = __byte_perm(w[2], w[3], 0x7362);
+    w[0] = __byte_perm(a, c, 0x5410); w[1] = __byte_perm(a, c, 0x7632);
+    w[2] = __byte_perm(b, d, 0x5410); w[3] = __byte_perm(b, d, 0x7632);
+}
+
+// Eight elements of a row as raw 16-byte vectors.
+template <class T> struct Raw { static constexpr int N = sizeof(T) / 2; uint4 v[N]; };
+template <class T>
+__device__ __forceinline__ Raw<T> load8(const T* from, int real, bool vector)
+{
+    Raw<T> r;
+    if (vector) {
+#pragma unroll
+        for (int i = 0; i < Raw<T>::N; ++i) r.v[i] = real > 0 ? reinterpret_cast<const uint4*>(from)[i] : make_uint4(0, 0, 0, 0);
+    } else {
+        T e[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = i < real ? from[i] : from_float<T>(0.f);
+        memcpy(&r, e, sizeof r);
+    }
+    return r;
+}
+
+template <int BITS, bool V, class T>
+__device__ __forceinline__ void write_rows(const Params& p, const Side& s, int window, int chunk)
+{
+    const int lane = threadIdx.x & 31;
+    const Place at = find_place(p, 32 * chunk + lane);
+    float inv[8];
+    int zc[8];
+    const float4* par = reinterpret_cast<const float4*>(s.quant + ((int64_t)at.h * p.nu * 32 + at.ch));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float4 x = at.valid ? par[i] : make_float4(0.f, 0.f, 0.f, 0.f);
+        inv[2 * i] = x.x; zc[2 * i] = __float_as_int(x.y); inv[2 * i + 1] = x.z; zc[2 * i + 1] = __float_as_int(x.w);
+    }
+    constexpr int WORDS = BITS == 8 ? 2 : 1;               // a lane's (3 bits: of the first three lanes of a unit)
+    const bool writes = at.valid && (BITS == 3 ? at.w < 3 : at.real > 0);
+    const int word = BITS == 8 ? 2 * at.w : at.w;
+    const int first = window * p.window;
+    Window groups = find_groups(p, first);
+    for (uint32_t left = groups.leaders; left; left &= left - 1) {
+        const int l = __ffs(left) - 1, n = __shfl_sync(0xffffffffu, groups.n, l);
+        const int64_t slot = __shfl_sync(0xffffffffu, groups.slot, l), page = page_of(slot, p.P);
+        const int key = (int)(slot - page * p.P), r = key % SLAB;
+        uint8_t* slab = s.pages + slab_offset(page, s.page_bytes, at.h, p.P / SLAB, key / SLAB, s.slab_bytes);
+        const T* row = static_cast<const T*>(s.rows) + (int64_t)(first + l) * s.ld + at.h * p.d + at.ch;
+        Raw<T> raw[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (k < n) raw[k] = load8(row + k * s.ld, at.real, s.vector);
+        uint32_t w[WORDS][4] = {};                         // of four tokens
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (k >= n) break;
+            T x[8];
+            memcpy(x, &raw[k], sizeof x);
+            int v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = quant_int(__fmaf_rn(to_float(x[i]), inv[i], 12582912.0f), zc[i]);
+            if constexpr (BITS == 8) {
+                w[0][k] = sat_pack_u8(v[1], v[0], sat_pack_u8(v[3], v[2], 0u));
+                w[1][k] = sat_pack_u8(v[5], v[4], sat_pack_u8(v[7], v[6], 0u));
+            } else if constexpr (BITS == 4) {
+                w[0][k] = sat_nibble_word(v);
+            } else {
+                const uint32_t x7 = sat_nibble_word_max7(v), tail = __shfl_sync(0xffffffffu, x7, lane | 3);
+                w[0][k] = x7 | (((tail >> at.w) & 0x11111111u) << 3);
+            }
+        }
+        if (!writes) continue;
+        if constexpr (!V) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (k >= n) break;
+                uint8_t* to = slab + k_word<BITS>(p.nu, at.u, word, r + k);
+                if constexpr (BITS == 8) *reinterpret_cast<uint2*>(to) = make_uint2(w[0][k], w[1][k]);
+                else *reinterpret_cast<uint32_t*>(to) = w[0][k];
+            }
+        } else {
+#pragma unroll
+            for (int x = 0; x < WORDS; ++x) {
+                uint8_t* to = slab + v_byte<BITS>(at.u, word + x, 0, r);
+                if (n == 4) {
+                    transpose4(w[x]);
+                    *reinterpret_cast<uint4*>(to) = make_uint4(w[x][0], w[x][1], w[x][2], w[x][3]);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 3; ++k) {
+                        if (k >= n) break;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) to[4 * e + k] = (uint8_t)(w[x][k] >> (8 * e));
+                    }
+                }
+            }
+        }
+    }
+}
+
+template <int BITS, bool V, class T>
+__device__ __forceinline__ void read_rows(const Params& p, const Side& s, int window, int chunk)
+{
+    const int lane = threadIdx.x & 31;
+    const Place at = find_place(p, 32 * chunk + lane);
+    float scale[8], zero[8];                               // 2^23 + z
+    const float4* par = reinterpret_cast<const float4*>(s.value + ((int64_t)at.h * p.nu * 32 + at.ch));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float4 x = at.valid ? par[i] : make_float4(0.f, 0.f, 0.f, 0.f);
+        scale[2 * i] = x.x; zero[2 * i] = 8388608.0f + x.y; scale[2 * i + 1] = x.z; zero[2 * i + 1] = 8388608.0f + x.w;
+    }
+    constexpr int WORDS = BITS == 8 ? 2 : 1;
+    const bool reads = at.valid && (BITS == 3 ? at.w < 3 : at.real > 0);
+    const int word = BITS == 8 ? 2 * at.w : at.w;
+    const int first = window * p.window;
+    Window groups = find_groups(p, first);
+    for (uint32_t left = groups.leaders; left; left &= left - 1) {
+        const int l = __ffs(left) - 1, n = __shfl_sync(0xffffffffu, groups.n, l);
+        const int64_t slot = __shfl_sync(0xffffffffu, groups.slot, l), page = page_of(slot, p.P);
+        const int key = (int)(slot - page * p.P), r = key % SLAB;
+        const uint8_t* slab = s.pages + slab_offset(page, s.page_bytes, at.h, p.P / SLAB, key / SLAB, s.slab_bytes);
+        uint32_t w[WORDS][4] = {};                         // of four tokens
+        if (reads) {
+            if constexpr (!V) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    if (k >= n) break;
+                    const uint8_t* from = slab + k_word<BITS>(p.nu, at.u, word, r + k);
+                    if constexpr (BITS == 8) {
+                        const uint2 x = *reinterpret_cast<const uint2*>(from);
+                        w[0][k] = x.x; w[1][k] = x.y;
+                    } else {
+                        w[0][k] = *reinterpret_cast<const uint32_t*>(from);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int x = 0; x < WORDS; ++x) {
+                    // all four keys' bytes, whichever of them are wanted
+                    const uint4 y = *reinterpret_cast<const uint4*>(slab + v_byte<BITS>(at.u, word + x, 0, r & ~3));
+                    uint32_t t[4] = {y.x, y.y, y.z, y.w};
+                    transpose4(t);
+                    const int skip = r & 3;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) w[x][k] = skip == 0 ? t[k] : skip == 1 ? t[k < 3 ? k + 1 : 3] : skip == 2 ? t[k < 2 ? k + 2 : 3] : t[3];
+                }
+            }
+        }
+        T* row = static_cast<T*>(s.rows) + (int64_t)(first + l) * s.ld + at.h * p.d + at.ch;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (k >= n) break;
+            uint32_t q[2];                                 // codes as bytes
+            if constexpr (BITS == 8) {
+                q[0] = w[0][k]; q[1] = w[1][k];
+            } else {
+                uint32_t x = w[0][k];
+                if constexpr (BITS == 3) {
+                    uint32_t tail = 0u;
+#pragma unroll
+                    for (int j = 0; j < 3; ++j) tail |= ((__shfl_sync(0xffffffffu, x, (lane & ~3) + j) >> 3) & 0x11111111u) << j;
+                    x = at.w == 3 ? tail : x & 0x77777777u;
+                }
+                q[0] = x & 0x0F0F0F0Fu; q[1] = (x >> 4) & 0x0F0F0F0Fu;
+            }
+            T y[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float c = __uint_as_float(__byte_perm(q[i >> 2], 0x4B000000u, 0x7540u | (i & 3)));      // 2^23 + code
+                y[i] = from_float<T>((c - zero[i]) * scale[i]);
+            }
+            if (at.real == 0) continue;
+            T* to = row + k * s.ld;
+            if (s.vector) {
+                Raw<T> raw;
+                memcpy(&raw, y, sizeof raw);
+#pragma unroll
+                for (int i = 0; i < Raw<T>::N; ++i) reinterpret_cast<uint4*>(to)[i] = raw.v[i];
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (i < at.real) to[i] = y[i];
+            }
+        }
+    }
+}
+
+// blockIdx.y: K or V. A warp takes a window of tokens and a chunk of 256 channels.
+template <class T, bool WRITE>
+__global__ void __launch_bounds__(THREADS) rows_kernel(const Params p)
+{
+    pdl_trigger();
+    pdl_wait();
+    const int n_chunks = (p.H * p.nu * 4 + 31) / 32;
+    const int64_t id = (int64_t)blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5);
+    const int64_t window = id / n_chunks;
+    if (window * p.window >= p.n_tokens) return;
+    const int w = (int)window, chunk = (int)(id - window * n_chunks);
+    const Side& s = p.side[blockIdx.y];
+    auto run = [&](auto bits) {
+        constexpr int BITS = decltype(bits)::value;
+        if (blockIdx.y == 0) {
+            if constexpr (WRITE) write_rows<BITS, false, T>(p, s, w, chunk);
+            else read_rows<BITS, false, T>(p, s, w, chunk);
+        } else {
+            if constexpr (WRITE) write_rows<BITS, true, T>(p, s, w, chunk);
+            else read_rows<BITS, true, T>(p, s, w, chunk);
+        }
+    };
+    if (s.bits == 3) run(std::integral_constant<int, 3>());
+    else if (s.bits == 4) run(std::integral_constant<int, 4>());
+    else run(std::integral_constant<int, 8>());
+}
+
+// ---------------------------------------------------------------- code rows
 template <int BITS>
 __device__ __forceinline__ void store_unit(uint8_t* slab, bool is_v, int nu, int u, int r, const uint32_t (&w)[BITS])
 {
@@ -83,24 +351,9 @@ __device__ __forceinline__ void store_unit(uint8_t* slab, bool is_v, int nu, int
         }
     }
 }
-template <int BITS>
-__device__ __forceinline__ void load_unit(const uint8_t* slab, bool is_v, int nu, int u, int r, uint32_t (&w)[BITS])
-{
-#pragma unroll
-    for (int i = 0; i < BITS; ++i) {
-        if (is_v) {
-            w[i] = 0;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) w[i] |= (uint32_t)slab[v_byte<BITS>(u, i, e, r)] << (8 * e);
-        } else {
-            w[i] = *reinterpret_cast<const uint32_t*>(slab + k_word<BITS>(nu, u, i, r));
-        }
-    }
-}
-
 // One thread per unit of a token's head.
-template <int BITS, class T, bool CODES>
-__device__ void write_units(const Params& p, const Side& s, bool is_v)
+template <int BITS>
+__device__ void write_code_rows(const Params& p, const Side& s, bool is_v)
 {
     const int64_t n = (int64_t)p.n_tokens * p.H * p.nu;
     for (int64_t i = (int64_t)blockIdx.x * THREADS + threadIdx.x; i < n; i += (int64_t)gridDim.x * THREADS) {
@@ -109,57 +362,14 @@ __device__ void write_units(const Params& p, const Side& s, bool is_v)
         if (!find_slot(p, token, page, key)) continue;
         uint32_t q[32], w[BITS];
         const int ch0 = h * p.d + 32 * u, real = min(32, p.d - 32 * u);
-        if constexpr (CODES) {
-            const uint8_t* row = static_cast<const uint8_t*>(s.rows) + (int64_t)token * s.ld;
+        const uint8_t* row = static_cast<const uint8_t*>(s.rows) + (int64_t)token * s.ld;
 #pragma unroll
-            for (int c = 0; c < 32; ++c) q[c] = c < real ? row_code<BITS>(row, s.pos[ch0 + c]) : 0u;
-            pack32<BITS>(q, w);
-        } else {
-            const T* row = static_cast<const T*>(s.rows) + (int64_t)token * s.ld + ch0;
-            const float2* par = s.quant + (int64_t)hu * 32;
-            int v[32];
-#pragma unroll
-            for (int c = 0; c < 32; ++c) {
-                const float2 a = par[c];
-                v[c] = quant_int(__fmaf_rn(c < real ? to_float(row[c]) : 0.f, a.x, 12582912.0f), __float_as_int(a.y));
-            }
-            pack32_sat<BITS>(v, w);
-        }
+        for (int c = 0; c < 32; ++c) q[c] = c < real ? row_code<BITS>(row, s.pos[ch0 + c]) : 0u;
+        pack32<BITS>(q, w);
         store_unit<BITS>(s.pages + slab_offset(page, s.page_bytes, h, p.P / SLAB, key / SLAB, s.slab_bytes), is_v, p.nu, u, key % SLAB, w);
     }
 }
-template <class T, bool CODES>
-__global__ void __launch_bounds__(THREADS) write_kernel(const Params p)
-{
-    pdl_trigger();
-    pdl_wait();
-    const bool is_v = blockIdx.y != 0;
-    const Side& s = p.side[blockIdx.y];
-    if (s.bits == 3) write_units<3, T, CODES>(p, s, is_v);
-    else if (s.bits == 4) write_units<4, T, CODES>(p, s, is_v);
-    else write_units<8, T, CODES>(p, s, is_v);
-}
-
-template <int BITS, class T>
-__device__ void read_units(const Params& p, const Side& s, bool is_v)
-{
-    const int64_t n = (int64_t)p.n_tokens * p.H * p.nu;
-    for (int64_t i = (int64_t)blockIdx.x * THREADS + threadIdx.x; i < n; i += (int64_t)gridDim.x * THREADS) {
-        const int token = (int)(i / (p.H * p.nu)), hu = (int)(i - (int64_t)token * (p.H * p.nu)), h = hu / p.nu, u = hu - h * p.nu;
-        int64_t page; int key;
-        if (!find_slot(p, token, page, key)) continue;
-        uint32_t w[BITS], o[8];
-        load_unit<BITS>(s.pages + slab_offset(page, s.page_bytes, h, p.P / SLAB, key / SLAB, s.slab_bytes), is_v, p.nu, u, key % SLAB, w);
-        unpack_act32<BITS>(w, o);
-        const int ch0 = h * p.d + 32 * u, real = min(32, p.d - 32 * u);
-        const float2* par = s.value + (int64_t)hu * 32;
-        T* row = static_cast<T*>(s.rows) + (int64_t)token * s.ld + ch0;
-#pragma unroll
-        for (int c = 0; c < 32; ++c)
-            if (c < real) row[c] = from_float<T>(((float)((o[c >> 2] >> (8 * (c & 3))) & 255u) - par[c].y) * par[c].x);
-    }
-}
-// Code rows: one thread per unit of the padded row.
+// One thread per unit of the padded row.
 template <int BITS>
 __device__ void read_code_rows(const Params& p, const Side& s, bool is_v)
 {
@@ -189,22 +399,43 @@ __device__ void read_code_rows(const Params& p, const Side& s, bool is_v)
         for (int k = 0; k < BITS; ++k) out[k] = w[k];
     }
 }
-template <class T, bool CODES>
-__global__ void __launch_bounds__(THREADS) read_kernel(const Params p)
+template <bool WRITE>
+__global__ void __launch_bounds__(THREADS) code_rows_kernel(const Params p)
 {
     pdl_trigger();
     pdl_wait();
     const bool is_v = blockIdx.y != 0;
     const Side& s = p.side[blockIdx.y];
-    if constexpr (CODES) {
+    if constexpr (WRITE) {
+        if (s.bits == 3) write_code_rows<3>(p, s, is_v);
+        else if (s.bits == 4) write_code_rows<4>(p, s, is_v);
+        else write_code_rows<8>(p, s, is_v);
+    } else {
         if (s.bits == 3) read_code_rows<3>(p, s, is_v);
         else if (s.bits == 4) read_code_rows<4>(p, s, is_v);
         else read_code_rows<8>(p, s, is_v);
-    } else {
-        if (s.bits == 3) read_units<3, T>(p, s, is_v);
-        else if (s.bits == 4) read_units<4, T>(p, s, is_v);
-        else read_units<8, T>(p, s, is_v);
     }
+}
+
+// Tokens per warp: as many as leave WARPS_PER_SM warps for every SM, and at least the four that go together when there are four.
+constexpr int WARPS_PER_SM = 32;
+template <bool WRITE>
+static int launch_rows(Params& p, int rows_type, int n_sm, cudaStream_t st)
+{
+    if (rows_type == RPTQ_ROWS_CODES) {
+        const int units = WRITE ? p.H * p.nu : p.side[0].n_units_row > p.side[1].n_units_row ? p.side[0].n_units_row : p.side[1].n_units_row;
+        const int64_t want = ((int64_t)p.n_tokens * units + THREADS - 1) / THREADS, most = (int64_t)n_sm * 16;
+        return launch_kernel(code_rows_kernel<WRITE>, dim3((unsigned)(want < most ? want : most), 2), THREADS, 0, 0, st, p);
+    }
+    const int64_t n_chunks = (p.H * p.nu * 4 + 31) / 32;
+    p.window = 32;
+    while (p.window > 1 && (int64_t)((p.n_tokens + p.window - 1) / p.window) * n_chunks * 2 < (int64_t)n_sm * WARPS_PER_SM) p.window /= 2;
+    const int64_t warps = (int64_t)((p.n_tokens + p.window - 1) / p.window) * n_chunks, blocks = (warps + THREADS / 32 - 1) / (THREADS / 32);
+    if (blocks > INT_MAX) return RPTQ_ERR_UNSUPPORTED;
+    const dim3 grid((unsigned)blocks, 2);
+    if (rows_type == RPTQ_ROWS_F32) return launch_kernel(rows_kernel<float, WRITE>, grid, THREADS, 0, 0, st, p);
+    if (rows_type == RPTQ_ROWS_F16) return launch_kernel(rows_kernel<__half, WRITE>, grid, THREADS, 0, 0, st, p);
+    return launch_kernel(rows_kernel<__nv_bfloat16, WRITE>, grid, THREADS, 0, 0, st, p);
 }
 
 static int element_bytes(int rows_type) { return rows_type == RPTQ_ROWS_F32 ? 4 : rows_type == RPTQ_ROWS_CODES ? 1 : 2; }
@@ -240,9 +471,9 @@ static int make_params(const rptq_kv_cache_t* c, const void* k, int64_t ldk, con
         s.pages = static_cast<uint8_t*>(const_cast<void*>(t ? v_pages : k_pages));
         s.rows = const_cast<void*>(t ? v : k);
         s.ld = t ? ldv : ldk;
-        s.vector = aligned16(s.rows) && (s.ld * e) % 16 == 0 && (c->d * e) % 16 == 0;
+        s.vector = aligned16(s.rows) && (s.ld * e) % 16 == 0 && c->d % 8 == 0;
     }
-    p->slots = slots; p->n_tokens = n_tokens; p->H = c->H; p->d = c->d; p->nu = c->nu; p->P = c->P; p->C = c->C;
+    p->slots = slots; p->n_tokens = n_tokens; p->H = c->H; p->d = c->d; p->nu = c->nu; p->P = c->P;
     p->n_slots = n_pages * c->P;
     p->status = device_status_word();
     return RPTQ_OK;
@@ -349,13 +580,7 @@ int rptq_kv_cache_write(const rptq_kv_cache_t* cache, const void* k, int64_t ldk
     int n_sm = 0;
     const int rc = make_params(cache, k, ldk, v, ldv, rows_type, slots, n_tokens, k_pages, v_pages, n_pages, &p, &nothing, &n_sm);
     if (rc != RPTQ_OK || nothing) return rc;
-    auto st = static_cast<cudaStream_t>(stream);
-    const int64_t want = ((int64_t)n_tokens * p.H * p.nu + THREADS - 1) / THREADS, most = (int64_t)n_sm * 16;
-    const dim3 grid((unsigned)(want < most ? want : most), 2);
-    if (rows_type == RPTQ_ROWS_F32) return launch_kernel(write_kernel<float, false>, grid, THREADS, 0, 0, st, p);
-    if (rows_type == RPTQ_ROWS_F16) return launch_kernel(write_kernel<__half, false>, grid, THREADS, 0, 0, st, p);
-    if (rows_type == RPTQ_ROWS_BF16) return launch_kernel(write_kernel<__nv_bfloat16, false>, grid, THREADS, 0, 0, st, p);
-    return launch_kernel(write_kernel<uint8_t, true>, grid, THREADS, 0, 0, st, p);
+    return launch_rows<true>(p, rows_type, n_sm, static_cast<cudaStream_t>(stream));
 }
 
 int rptq_kv_cache_read(const rptq_kv_cache_t* cache, const void* k_pages, const void* v_pages, int64_t n_pages, const int64_t* slots,
@@ -368,14 +593,7 @@ int rptq_kv_cache_read(const rptq_kv_cache_t* cache, const void* k_pages, const 
     int n_sm = 0;
     const int rc = make_params(cache, k, ldk, v, ldv, rows_type, slots, n_tokens, k_pages, v_pages, n_pages, &p, &nothing, &n_sm);
     if (rc != RPTQ_OK || nothing) return rc;
-    auto st = static_cast<cudaStream_t>(stream);
-    const int units = rows_type == RPTQ_ROWS_CODES ? (p.side[0].n_units_row > p.side[1].n_units_row ? p.side[0].n_units_row : p.side[1].n_units_row) : p.H * p.nu;
-    const int64_t want = ((int64_t)n_tokens * units + THREADS - 1) / THREADS, most = (int64_t)n_sm * 16;
-    const dim3 grid((unsigned)(want < most ? want : most), 2);
-    if (rows_type == RPTQ_ROWS_F32) return launch_kernel(read_kernel<float, false>, grid, THREADS, 0, 0, st, p);
-    if (rows_type == RPTQ_ROWS_F16) return launch_kernel(read_kernel<__half, false>, grid, THREADS, 0, 0, st, p);
-    if (rows_type == RPTQ_ROWS_BF16) return launch_kernel(read_kernel<__nv_bfloat16, false>, grid, THREADS, 0, 0, st, p);
-    return launch_kernel(read_kernel<uint8_t, true>, grid, THREADS, 0, 0, st, p);
+    return launch_rows<false>(p, rows_type, n_sm, static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

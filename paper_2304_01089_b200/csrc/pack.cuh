@@ -60,6 +60,12 @@ __device__ __forceinline__ uint32_t sat_nibble_word(const int* v)     // 8 integ
     d = sat_pack_u4(v[5], v[1], d);
     return sat_pack_u4(v[4], v[0], d);
 }
+// the same of 3-bit codes (bit 3 of every nibble 0): nibbles above 7 become 7, eight at a time
+__device__ __forceinline__ uint32_t sat_nibble_word_max7(const int* v)
+{
+    const uint32_t x = sat_nibble_word(v);
+    return (x | (((x >> 3) & 0x11111111u) * 7u)) & 0x77777777u;
+}
 template <int BITS>
 __device__ __forceinline__ void pack32_sat(const int (&v)[32], uint32_t (&w)[BITS], uint32_t flip = 0u)
 {
