@@ -16,6 +16,7 @@
 
 #include "kv_pages.cuh"
 #include "pack.cuh"
+#include "tc.cuh"
 #include "unpack.cuh"
 
 namespace rptq {
@@ -40,7 +41,7 @@ struct Params {
     Side side[2];                  // K, V
     const int64_t* slots;
     int n_tokens, H, d, nu, P;
-    int window;                    // tokens a warp looks at, 1 .. 32
+    int window;                    // tokens of a warp, 1 .. 32
     int64_t n_slots;
     int* status;
 };
@@ -61,9 +62,6 @@ __device__ __forceinline__ bool find_slot(const Params& p, int token, int64_t& p
     return true;
 }
 
-__device__ __forceinline__ float to_float(float x) { return x; }
-__device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
-__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
 template <class T> __device__ __forceinline__ T from_float(float x);
 template <> __device__ __forceinline__ float from_float<float>(float x) { return x; }
 template <> __device__ __forceinline__ __half from_float<__half>(float x) { return __float2half_rn(x); }
@@ -82,36 +80,46 @@ __device__ __forceinline__ uint32_t row_code(const uint8_t* row, int pos)
 }
 
 // ---------------------------------------------------------------- rows of values
-// The tokens of a warp's window that go together: lane l stands for token first + l. A token leads when it is the first of its call in a
+// The tokens that go together among first .. end - 1, at most 32: lane l stands for token first + l. A token leads when it is the first of its call in a
 // group of four keys whose slots follow one another; `n` tokens from it on are its group.
-struct Window { int64_t slot; int n; uint32_t leaders; };
-__device__ __forceinline__ Window find_groups(const Params& p, int first)
+struct Window {
+    int64_t at;                    // byte of the token's slab of head 0 in the pool
+    int key_n;                     // 8 (key in the slab) + n
+    uint32_t leaders;
+};
+__device__ __forceinline__ Window find_groups(const Params& p, const Side& s, int first, int end)
 {
     const int lane = threadIdx.x & 31, i = first + lane;
-    Window w{-1, 0, 0u};
+    Window w{0, 0, 0u};
     bool leads = false;
-    if (lane < p.window && i < p.n_tokens) {
-        const int64_t s = p.slots[i];
-        if (s >= p.n_slots) {
+    if (i < end) {
+        const int64_t slot = p.slots[i];
+        if (slot >= p.n_slots) {
             if (p.status) *p.status = RPTQ_ERR_BAD_SLOT;
-        } else if (s >= 0) {
-            const int in_four = (int)(s & 3);
-            leads = in_four == 0 || i == 0 || p.slots[i - 1] != s - 1;
-            w.slot = s;
-            w.n = 1;
-            while (leads && in_four + w.n < 4 && i + w.n < p.n_tokens && p.slots[i + w.n] == s + w.n && s + w.n < p.n_slots) ++w.n;
+        } else if (slot >= 0) {
+            const int in_four = (int)(slot & 3);
+            leads = in_four == 0 || i == 0 || p.slots[i - 1] != slot - 1;
+            int n = 1;
+            while (leads && in_four + n < 4 && i + n < p.n_tokens && p.slots[i + n] == slot + n && slot + n < p.n_slots) ++n;
+            const int64_t page = page_of(slot, p.P);
+            const int key = (int)(slot - page * p.P);
+            w.at = page * s.page_bytes + (int64_t)(key / SLAB) * s.slab_bytes;
+            w.key_n = 8 * (key % SLAB) + n;
         }
     }
     w.leaders = __ballot_sync(0xffffffffu, leads);
     return w;
 }
 // Eight channels of a head: the lane's place among all heads' groups of eight.
-struct Place { int h, u, w, ch, real; bool valid; };       // unit, group of the unit, first channel of the head, channels that exist
+struct Place {
+    int h, u, w, ch, real;         // head, unit, group of the unit, first channel in the head, channels that exist
+    bool valid;
+};
 __device__ __forceinline__ Place find_place(const Params& p, int group)
 {
     Place x;
     x.valid = group < p.H * p.nu * 4;
-    const int unit = group >> 2;
+    const int unit = x.valid ? group >> 2 : 0;
     x.h = unit / p.nu;
     x.u = unit - x.h * p.nu;
     x.w = group & 3;
@@ -130,11 +138,13 @@ __device__ __forceinline__ void transpose4(uint32_t (&w)[4])
 
 // Eight elements of a row as raw 16-byte vectors.
 template <class T> struct Raw { static constexpr int N = sizeof(T) / 2; uint4 v[N]; };
-template <class T>
-__device__ __forceinline__ Raw<T> load8(const T* from, int real, bool vector)
+template <class T> struct Rows { Raw<T> of[4]; };                   // of four tokens
+template <int N> struct Words { uint32_t w[N][4]; };                // N words of four tokens
+template <class T, bool VECTOR>
+__device__ __forceinline__ Raw<T> load8(const T* from, int real)
 {
     Raw<T> r;
-    if (vector) {
+    if constexpr (VECTOR) {
 #pragma unroll
         for (int i = 0; i < Raw<T>::N; ++i) r.v[i] = real > 0 ? reinterpret_cast<const uint4*>(from)[i] : make_uint4(0, 0, 0, 0);
     } else {
@@ -145,44 +155,64 @@ __device__ __forceinline__ Raw<T> load8(const T* from, int real, bool vector)
     }
     return r;
 }
+// Elements 2 i, 2 i + 1.
+template <class T> __device__ __forceinline__ float2 pair_of(const Raw<T>& r, int i);
+template <> __device__ __forceinline__ float2 pair_of(const Raw<float>& r, int i)
+{
+    const uint4 v = r.v[i >> 1];
+    return i & 1 ? make_float2(__uint_as_float(v.z), __uint_as_float(v.w)) : make_float2(__uint_as_float(v.x), __uint_as_float(v.y));
+}
+__device__ __forceinline__ uint32_t word_of(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
+template <> __device__ __forceinline__ float2 pair_of(const Raw<__half>& r, int i)
+{
+    const uint32_t w = word_of(r.v[0], i);
+    return __half22float2(*reinterpret_cast<const __half2*>(&w));
+}
+template <> __device__ __forceinline__ float2 pair_of(const Raw<__nv_bfloat16>& r, int i)
+{
+    const uint32_t w = word_of(r.v[0], i);
+    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+}
+// Two numbers into elements 2 i, 2 i + 1.
+__device__ __forceinline__ uint32_t join2(float2 x, __half) { const __half2 h = __float22half2_rn(x); return *reinterpret_cast<const uint32_t*>(&h); }
+__device__ __forceinline__ uint32_t join2(float2 x, __nv_bfloat16) { const __nv_bfloat162 h = __float22bfloat162_rn(x); return *reinterpret_cast<const uint32_t*>(&h); }
 
 template <int BITS, bool V, class T>
-__device__ __forceinline__ void write_rows(const Params& p, const Side& s, int window, int chunk)
+__device__ __forceinline__ void write_rows(const Params& p, const Side& s, int first, int end, int chunk)
 {
     const int lane = threadIdx.x & 31;
     const Place at = find_place(p, 32 * chunk + lane);
-    float inv[8];
+    float2 inv[4];
     int zc[8];
     const float4* par = reinterpret_cast<const float4*>(s.quant + ((int64_t)at.h * p.nu * 32 + at.ch));
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const float4 x = at.valid ? par[i] : make_float4(0.f, 0.f, 0.f, 0.f);
-        inv[2 * i] = x.x; zc[2 * i] = __float_as_int(x.y); inv[2 * i + 1] = x.z; zc[2 * i + 1] = __float_as_int(x.w);
+        const float4 x = par[i];
+        inv[i] = make_float2(x.x, x.z); zc[2 * i] = __float_as_int(x.y); zc[2 * i + 1] = __float_as_int(x.w);
     }
     constexpr int WORDS = BITS == 8 ? 2 : 1;               // a lane's (3 bits: of the first three lanes of a unit)
     const bool writes = at.valid && (BITS == 3 ? at.w < 3 : at.real > 0);
     const int word = BITS == 8 ? 2 * at.w : at.w;
-    const int first = window * p.window;
-    Window groups = find_groups(p, first);
-    for (uint32_t left = groups.leaders; left; left &= left - 1) {
-        const int l = __ffs(left) - 1, n = __shfl_sync(0xffffffffu, groups.n, l);
-        const int64_t slot = __shfl_sync(0xffffffffu, groups.slot, l), page = page_of(slot, p.P);
-        const int key = (int)(slot - page * p.P), r = key % SLAB;
-        uint8_t* slab = s.pages + slab_offset(page, s.page_bytes, at.h, p.P / SLAB, key / SLAB, s.slab_bytes);
-        const T* row = static_cast<const T*>(s.rows) + (int64_t)(first + l) * s.ld + at.h * p.d + at.ch;
-        Raw<T> raw[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if (k < n) raw[k] = load8(row + k * s.ld, at.real, s.vector);
-        uint32_t w[WORDS][4] = {};                         // of four tokens
+    // my first word of key 0 of the head's first slab, and the bytes between keys
+    uint8_t* const mine = s.pages + slab_offset(0, 0, at.h, p.P / SLAB, 0, s.slab_bytes) + (V ? v_byte<BITS>(at.u, writes ? word : 0, 0, 0) : k_word<BITS>(p.nu, at.u, writes ? word : 0, 0));
+    const int key_step = V ? 0 : k_word<BITS>(p.nu, at.u, 0, 1) - k_word<BITS>(p.nu, at.u, 0, 0);
+    const T* const row0 = static_cast<const T*>(s.rows) + (int64_t)first * s.ld + at.h * p.d + at.ch;
+    const Window groups = find_groups(p, s, first, end);
+
+    // n tokens; FOUR: n == 4
+    auto group = [&](const Rows<T>& rows, uint8_t* slab, int r, int n, auto four) {
+        constexpr bool FOUR = decltype(four)::value;
+        uint32_t w[WORDS][4] = {};
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            if (k >= n) break;
-            T x[8];
-            memcpy(x, &raw[k], sizeof x);
+            if (!FOUR && k >= n) break;
             int v[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = quant_int(__fmaf_rn(to_float(x[i]), inv[i], 12582912.0f), zc[i]);
+            for (int i = 0; i < 4; ++i) {
+                const float2 t = tc::fma2(pair_of(rows.of[k], i), inv[i], make_float2(12582912.0f, 12582912.0f));
+                v[2 * i] = quant_int(t.x, zc[2 * i]);
+                v[2 * i + 1] = quant_int(t.y, zc[2 * i + 1]);
+            }
             if constexpr (BITS == 8) {
                 w[0][k] = sat_pack_u8(v[1], v[0], sat_pack_u8(v[3], v[2], 0u));
                 w[1][k] = sat_pack_u8(v[5], v[4], sat_pack_u8(v[7], v[6], 0u));
@@ -193,93 +223,123 @@ __device__ __forceinline__ void write_rows(const Params& p, const Side& s, int w
                 w[0][k] = x7 | (((tail >> at.w) & 0x11111111u) << 3);
             }
         }
-        if (!writes) continue;
+        if (!writes) return;
         if constexpr (!V) {
+            uint8_t* to = slab + r * key_step;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                if (k >= n) break;
-                uint8_t* to = slab + k_word<BITS>(p.nu, at.u, word, r + k);
+            for (int k = 0; k < 4; ++k, to += key_step) {
+                if (!FOUR && k >= n) break;
                 if constexpr (BITS == 8) *reinterpret_cast<uint2*>(to) = make_uint2(w[0][k], w[1][k]);
                 else *reinterpret_cast<uint32_t*>(to) = w[0][k];
             }
         } else {
+            uint8_t* to = slab + 16 * (r >> 2) + (r & 3);
 #pragma unroll
             for (int x = 0; x < WORDS; ++x) {
-                uint8_t* to = slab + v_byte<BITS>(at.u, word + x, 0, r);
-                if (n == 4) {
+                if constexpr (FOUR) {
                     transpose4(w[x]);
-                    *reinterpret_cast<uint4*>(to) = make_uint4(w[x][0], w[x][1], w[x][2], w[x][3]);
+                    *reinterpret_cast<uint4*>(to + 64 * x) = make_uint4(w[x][0], w[x][1], w[x][2], w[x][3]);
                 } else {
 #pragma unroll
-                    for (int k = 0; k < 3; ++k) {
+                    for (int k = 0; k < 4; ++k) {
                         if (k >= n) break;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) to[4 * e + k] = (uint8_t)(w[x][k] >> (8 * e));
+                        for (int e = 0; e < 4; ++e) to[64 * x + 4 * e + k] = (uint8_t)(w[x][k] >> (8 * e));
                     }
                 }
             }
         }
+    };
+    // a group's rows are on their way while the one before is quantised
+    Rows<T> rows, ahead;
+    uint32_t left = groups.leaders;
+    auto load = [&](Rows<T>& to) {
+        const int l = __ffs(left) - 1, n = __shfl_sync(0xffffffffu, groups.key_n, l) & 7;
+        const T* row = row0 + (int64_t)l * s.ld;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (k < n) to.of[k] = s.vector ? load8<T, true>(row + k * s.ld, at.real) : load8<T, false>(row + k * s.ld, at.real);
+    };
+    if (left) load(rows);
+    while (left) {
+        const int l = __ffs(left) - 1, key_n = __shfl_sync(0xffffffffu, groups.key_n, l), r = key_n >> 3, n = key_n & 7;
+        uint8_t* slab = mine + __shfl_sync(0xffffffffu, groups.at, l);
+        left &= left - 1;
+        if (left) load(ahead);
+        if (n == 4) group(rows, slab, r, n, std::true_type());
+        else group(rows, slab, r, n, std::false_type());
+        rows = ahead;
     }
 }
 
 template <int BITS, bool V, class T>
-__device__ __forceinline__ void read_rows(const Params& p, const Side& s, int window, int chunk)
+__device__ __forceinline__ void read_rows(const Params& p, const Side& s, int first, int end, int chunk)
 {
     const int lane = threadIdx.x & 31;
     const Place at = find_place(p, 32 * chunk + lane);
-    float scale[8], zero[8];                               // 2^23 + z
+    float2 scale[4], zero[4];                              // zero: -(2^23 + z)
     const float4* par = reinterpret_cast<const float4*>(s.value + ((int64_t)at.h * p.nu * 32 + at.ch));
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const float4 x = at.valid ? par[i] : make_float4(0.f, 0.f, 0.f, 0.f);
-        scale[2 * i] = x.x; zero[2 * i] = 8388608.0f + x.y; scale[2 * i + 1] = x.z; zero[2 * i + 1] = 8388608.0f + x.w;
+        const float4 x = par[i];
+        scale[i] = make_float2(x.x, x.z); zero[i] = make_float2(-8388608.0f - x.y, -8388608.0f - x.w);
     }
     constexpr int WORDS = BITS == 8 ? 2 : 1;
     const bool reads = at.valid && (BITS == 3 ? at.w < 3 : at.real > 0);
     const int word = BITS == 8 ? 2 * at.w : at.w;
-    const int first = window * p.window;
-    Window groups = find_groups(p, first);
-    for (uint32_t left = groups.leaders; left; left &= left - 1) {
-        const int l = __ffs(left) - 1, n = __shfl_sync(0xffffffffu, groups.n, l);
-        const int64_t slot = __shfl_sync(0xffffffffu, groups.slot, l), page = page_of(slot, p.P);
-        const int key = (int)(slot - page * p.P), r = key % SLAB;
-        const uint8_t* slab = s.pages + slab_offset(page, s.page_bytes, at.h, p.P / SLAB, key / SLAB, s.slab_bytes);
-        uint32_t w[WORDS][4] = {};                         // of four tokens
+    const uint8_t* const mine = s.pages + slab_offset(0, 0, at.h, p.P / SLAB, 0, s.slab_bytes) + (V ? v_byte<BITS>(at.u, reads ? word : 0, 0, 0) : k_word<BITS>(p.nu, at.u, reads ? word : 0, 0));
+    const int key_step = V ? 0 : k_word<BITS>(p.nu, at.u, 0, 1) - k_word<BITS>(p.nu, at.u, 0, 0);
+    T* const row0 = static_cast<T*>(s.rows) + (int64_t)first * s.ld + at.h * p.d + at.ch;
+    const Window groups = find_groups(p, s, first, end);
+
+    auto load = [&](Words<WORDS>& to, int l) {
+        const int key_n = __shfl_sync(0xffffffffu, groups.key_n, l), r = key_n >> 3, n = key_n & 7;
+        const uint8_t* slab = mine + __shfl_sync(0xffffffffu, groups.at, l);
         if (reads) {
             if constexpr (!V) {
+                const uint8_t* from = slab + r * key_step;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
+                for (int k = 0; k < 4; ++k, from += key_step) {
                     if (k >= n) break;
-                    const uint8_t* from = slab + k_word<BITS>(p.nu, at.u, word, r + k);
                     if constexpr (BITS == 8) {
                         const uint2 x = *reinterpret_cast<const uint2*>(from);
-                        w[0][k] = x.x; w[1][k] = x.y;
+                        to.w[0][k] = x.x; to.w[1][k] = x.y;
                     } else {
-                        w[0][k] = *reinterpret_cast<const uint32_t*>(from);
+                        to.w[0][k] = *reinterpret_cast<const uint32_t*>(from);
                     }
                 }
             } else {
 #pragma unroll
                 for (int x = 0; x < WORDS; ++x) {
                     // all four keys' bytes, whichever of them are wanted
-                    const uint4 y = *reinterpret_cast<const uint4*>(slab + v_byte<BITS>(at.u, word + x, 0, r & ~3));
-                    uint32_t t[4] = {y.x, y.y, y.z, y.w};
-                    transpose4(t);
-                    const int skip = r & 3;
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) w[x][k] = skip == 0 ? t[k] : skip == 1 ? t[k < 3 ? k + 1 : 3] : skip == 2 ? t[k < 2 ? k + 2 : 3] : t[3];
+                    const uint4 y = *reinterpret_cast<const uint4*>(slab + 64 * x + 16 * (r >> 2));
+                    to.w[x][0] = y.x; to.w[x][1] = y.y; to.w[x][2] = y.z; to.w[x][3] = y.w;
                 }
             }
         }
-        T* row = static_cast<T*>(s.rows) + (int64_t)(first + l) * s.ld + at.h * p.d + at.ch;
+    };
+    auto group = [&](Words<WORDS> words, T* row, int r, int n, auto four, auto vector) {
+        constexpr bool FOUR = decltype(four)::value, VECTOR = decltype(vector)::value;
+        if constexpr (V) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            if (k >= n) break;
+            for (int x = 0; x < WORDS; ++x) {
+                uint32_t (&t)[4] = words.w[x];
+                transpose4(t);
+                if constexpr (!FOUR) {
+                    const int skip = r & 3;
+                    if (skip & 1) { t[0] = t[1]; t[1] = t[2]; t[2] = t[3]; }
+                    if (skip & 2) { t[0] = t[2]; t[1] = t[3]; }
+                }
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k, row += s.ld) {
+            if (!FOUR && k >= n) break;
             uint32_t q[2];                                 // codes as bytes
             if constexpr (BITS == 8) {
-                q[0] = w[0][k]; q[1] = w[1][k];
+                q[0] = words.w[0][k]; q[1] = words.w[1][k];
             } else {
-                uint32_t x = w[0][k];
+                uint32_t x = words.w[0][k];
                 if constexpr (BITS == 3) {
                     uint32_t tail = 0u;
 #pragma unroll
@@ -288,48 +348,69 @@ __device__ __forceinline__ void read_rows(const Params& p, const Side& s, int wi
                 }
                 q[0] = x & 0x0F0F0F0Fu; q[1] = (x >> 4) & 0x0F0F0F0Fu;
             }
-            T y[8];
+            float2 y[4];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float c = __uint_as_float(__byte_perm(q[i >> 2], 0x4B000000u, 0x7540u | (i & 3)));      // 2^23 + code
-                y[i] = from_float<T>((c - zero[i]) * scale[i]);
+            for (int i = 0; i < 4; ++i) {                  // 2^23 + code, exactly; minus 2^23 + z, exactly; one rounding with s
+                const uint32_t b = q[i >> 1];
+                const float2 c = make_float2(__uint_as_float(__byte_perm(b, 0x4B000000u, i & 1 ? 0x7542u : 0x7540u)),
+                                             __uint_as_float(__byte_perm(b, 0x4B000000u, i & 1 ? 0x7543u : 0x7541u)));
+                y[i] = tc::mul2(tc::add2(c, zero[i]), scale[i]);
             }
             if (at.real == 0) continue;
-            T* to = row + k * s.ld;
-            if (s.vector) {
-                Raw<T> raw;
-                memcpy(&raw, y, sizeof raw);
-#pragma unroll
-                for (int i = 0; i < Raw<T>::N; ++i) reinterpret_cast<uint4*>(to)[i] = raw.v[i];
+            if constexpr (VECTOR) {
+                if constexpr (std::is_same<T, float>::value) {
+                    reinterpret_cast<float4*>(row)[0] = make_float4(y[0].x, y[0].y, y[1].x, y[1].y);
+                    reinterpret_cast<float4*>(row)[1] = make_float4(y[2].x, y[2].y, y[3].x, y[3].y);
+                } else {
+                    *reinterpret_cast<uint4*>(row) = make_uint4(join2(y[0], T()), join2(y[1], T()), join2(y[2], T()), join2(y[3], T()));
+                }
             } else {
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
-                    if (i < at.real) to[i] = y[i];
+                    if (i < at.real) row[i] = from_float<T>(i & 1 ? y[i >> 1].y : y[i >> 1].x);
             }
         }
+    };
+    Words<WORDS> words{}, ahead{};
+    uint32_t left = groups.leaders;
+    if (left) load(words, __ffs(left) - 1);
+    while (left) {
+        const int l = __ffs(left) - 1, key_n = __shfl_sync(0xffffffffu, groups.key_n, l), r = key_n >> 3, n = key_n & 7;
+        T* row = row0 + (int64_t)l * s.ld;
+        left &= left - 1;
+        if (left) load(ahead, __ffs(left) - 1);
+        using Yes = std::true_type; using No = std::false_type;
+        if (!s.vector) group(words, row, r, n, No(), No());
+        else if (n == 4) group(words, row, r, n, Yes(), Yes());
+        else group(words, row, r, n, No(), Yes());
+        words = ahead;
     }
 }
 
-// blockIdx.y: K or V. A warp takes a window of tokens and a chunk of 256 channels.
+// A warp takes a chunk of 256 channels of K or V (blockIdx.y) and a window of the tokens; the four warps of a block take neighbouring
+// chunks. Six blocks per SM (80 registers; rows of fp32 four, 128). (Parts as long as make all warps resident at once, K's and V's at the same
+// time, were 15 % slower: 90 us against 77 for the longest timed case.)
+template <class T> constexpr int rows_blocks_per_sm() { return sizeof(T) == 4 ? 4 : 6; }
 template <class T, bool WRITE>
-__global__ void __launch_bounds__(THREADS) rows_kernel(const Params p)
+__global__ void __launch_bounds__(THREADS, rows_blocks_per_sm<T>()) rows_kernel(const Params p)
 {
     pdl_trigger();
     pdl_wait();
     const int n_chunks = (p.H * p.nu * 4 + 31) / 32;
-    const int64_t id = (int64_t)blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5);
-    const int64_t window = id / n_chunks;
+    const int64_t id = (int64_t)blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5), window = id / n_chunks;
+    const bool is_v = blockIdx.y != 0;
+    const int chunk = (int)(id - window * n_chunks);
     if (window * p.window >= p.n_tokens) return;
-    const int w = (int)window, chunk = (int)(id - window * n_chunks);
-    const Side& s = p.side[blockIdx.y];
+    const int first = (int)window * p.window, end = (int)min((int64_t)first + p.window, (int64_t)p.n_tokens);
+    const Side& s = p.side[is_v];
     auto run = [&](auto bits) {
         constexpr int BITS = decltype(bits)::value;
-        if (blockIdx.y == 0) {
-            if constexpr (WRITE) write_rows<BITS, false, T>(p, s, w, chunk);
-            else read_rows<BITS, false, T>(p, s, w, chunk);
+        if (!is_v) {
+            if constexpr (WRITE) write_rows<BITS, false, T>(p, s, first, end, chunk);
+            else read_rows<BITS, false, T>(p, s, first, end, chunk);
         } else {
-            if constexpr (WRITE) write_rows<BITS, true, T>(p, s, w, chunk);
-            else read_rows<BITS, true, T>(p, s, w, chunk);
+            if constexpr (WRITE) write_rows<BITS, true, T>(p, s, first, end, chunk);
+            else read_rows<BITS, true, T>(p, s, first, end, chunk);
         }
     };
     if (s.bits == 3) run(std::integral_constant<int, 3>());
@@ -417,8 +498,20 @@ __global__ void __launch_bounds__(THREADS) code_rows_kernel(const Params p)
     }
 }
 
-// Tokens per warp: as many as leave WARPS_PER_SM warps for every SM, and at least the four that go together when there are four.
-constexpr int WARPS_PER_SM = 32;
+// Tokens per warp: as many as leave WARPS_PER_SM warps for every SM. (Measured with 16, 32, 64, 128: 83, 83, 87, 96 us for the longest timed
+// case, 8.7, 9.3, 9.4, 9.3 for the shortest with several tokens.)
+constexpr int WARPS_PER_SM = 16;
+template <class T, bool WRITE>
+static int launch_values(Params& p, int n_sm, cudaStream_t st)
+{
+    const int64_t n_chunks = (p.H * p.nu * 4 + 31) / 32;
+    auto windows = [&]() { return ((int64_t)p.n_tokens + p.window - 1) / p.window; };
+    p.window = 32;
+    while (p.window > 1 && windows() * n_chunks * 2 < (int64_t)n_sm * WARPS_PER_SM) p.window /= 2;
+    const int64_t blocks = (windows() * n_chunks + THREADS / 32 - 1) / (THREADS / 32);
+    if (blocks > INT_MAX) return RPTQ_ERR_UNSUPPORTED;
+    return launch_kernel(rows_kernel<T, WRITE>, dim3((unsigned)blocks, 2), THREADS, 0, 0, st, p);
+}
 template <bool WRITE>
 static int launch_rows(Params& p, int rows_type, int n_sm, cudaStream_t st)
 {
@@ -427,15 +520,9 @@ static int launch_rows(Params& p, int rows_type, int n_sm, cudaStream_t st)
         const int64_t want = ((int64_t)p.n_tokens * units + THREADS - 1) / THREADS, most = (int64_t)n_sm * 16;
         return launch_kernel(code_rows_kernel<WRITE>, dim3((unsigned)(want < most ? want : most), 2), THREADS, 0, 0, st, p);
     }
-    const int64_t n_chunks = (p.H * p.nu * 4 + 31) / 32;
-    p.window = 32;
-    while (p.window > 1 && (int64_t)((p.n_tokens + p.window - 1) / p.window) * n_chunks * 2 < (int64_t)n_sm * WARPS_PER_SM) p.window /= 2;
-    const int64_t warps = (int64_t)((p.n_tokens + p.window - 1) / p.window) * n_chunks, blocks = (warps + THREADS / 32 - 1) / (THREADS / 32);
-    if (blocks > INT_MAX) return RPTQ_ERR_UNSUPPORTED;
-    const dim3 grid((unsigned)blocks, 2);
-    if (rows_type == RPTQ_ROWS_F32) return launch_kernel(rows_kernel<float, WRITE>, grid, THREADS, 0, 0, st, p);
-    if (rows_type == RPTQ_ROWS_F16) return launch_kernel(rows_kernel<__half, WRITE>, grid, THREADS, 0, 0, st, p);
-    return launch_kernel(rows_kernel<__nv_bfloat16, WRITE>, grid, THREADS, 0, 0, st, p);
+    if (rows_type == RPTQ_ROWS_F32) return launch_values<float, WRITE>(p, n_sm, st);
+    if (rows_type == RPTQ_ROWS_F16) return launch_values<__half, WRITE>(p, n_sm, st);
+    return launch_values<__nv_bfloat16, WRITE>(p, n_sm, st);
 }
 
 static int element_bytes(int rows_type) { return rows_type == RPTQ_ROWS_F32 ? 4 : rows_type == RPTQ_ROWS_CODES ? 1 : 2; }
