@@ -41,7 +41,7 @@ struct Params {
     Side side[2];                  // K, V
     const int64_t* slots;
     int n_tokens, H, d, nu, P;
-    int window;                    // tokens of a warp, 1 .. 32
+    int window;                    // tokens of a warp, 1 .. MAX_WINDOW
     int64_t n_slots;
     int* status;
 };
@@ -80,8 +80,9 @@ __device__ __forceinline__ uint32_t row_code(const uint8_t* row, int pos)
 }
 
 // ---------------------------------------------------------------- rows of values
-// The tokens that go together among first .. end - 1, at most 32: lane l stands for token first + l. A token leads when it is the first of its call in a
-// group of four keys whose slots follow one another; `n` tokens from it on are its group.
+// The tokens that go together among first .. end - 1, at most MAX_WINDOW: lane l stands for token first + l. A token leads when it is the
+// first of its call in a group of four keys whose slots follow one another; `n` tokens from it on are its group.
+constexpr int MAX_WINDOW = 16;
 struct Window {
     int64_t at;                    // byte of the token's slab of head 0 in the pool
     int key_n;                     // 8 (key in the slab) + n
@@ -90,17 +91,22 @@ struct Window {
 __device__ __forceinline__ Window find_groups(const Params& p, const Side& s, int first, int end)
 {
     const int lane = threadIdx.x & 31, i = first + lane;
+    const int64_t before = i > 0 && i <= p.n_tokens ? p.slots[i - 1] : -2;     // the one load: a lane's slot is the next lane's `before`
+    const int64_t slot = __shfl_down_sync(0xffffffffu, before, 1);
+    const int in_four = (int)(slot & 3);
+    int n = 1;
+#pragma unroll
+    for (int k = 1; k < 4; ++k) {
+        const int64_t next = __shfl_down_sync(0xffffffffu, before, 1 + k);
+        if (n == k && in_four + k < 4 && next == slot + k && next < p.n_slots) ++n;
+    }
     Window w{0, 0, 0u};
     bool leads = false;
-    if (i < end) {
-        const int64_t slot = p.slots[i];
+    if (i < end && slot >= 0) {
         if (slot >= p.n_slots) {
             if (p.status) *p.status = RPTQ_ERR_BAD_SLOT;
-        } else if (slot >= 0) {
-            const int in_four = (int)(slot & 3);
-            leads = in_four == 0 || i == 0 || p.slots[i - 1] != slot - 1;
-            int n = 1;
-            while (leads && in_four + n < 4 && i + n < p.n_tokens && p.slots[i + n] == slot + n && slot + n < p.n_slots) ++n;
+        } else {
+            leads = in_four == 0 || before != slot - 1;
             const int64_t page = page_of(slot, p.P);
             const int key = (int)(slot - page * p.P);
             w.at = page * s.page_bytes + (int64_t)(key / SLAB) * s.slab_bytes;
@@ -284,6 +290,7 @@ __device__ __forceinline__ void read_rows(const Params& p, const Side& s, int fi
         const float4 x = par[i];
         scale[i] = make_float2(x.x, x.z); zero[i] = make_float2(-8388608.0f - x.y, -8388608.0f - x.w);
     }
+    pdl_wait();                                            // (the handle's tables were there before any launch)
     constexpr int WORDS = BITS == 8 ? 2 : 1;
     const bool reads = at.valid && (BITS == 3 ? at.w < 3 : at.real > 0);
     const int word = BITS == 8 ? 2 * at.w : at.w;
@@ -395,12 +402,12 @@ template <class T, bool WRITE>
 __global__ void __launch_bounds__(THREADS, rows_blocks_per_sm<T>()) rows_kernel(const Params p)
 {
     pdl_trigger();
-    pdl_wait();
+    if constexpr (WRITE) pdl_wait();                       // (inside, behind the loads of the parameters, it costs the write's instances registers)
     const int n_chunks = (p.H * p.nu * 4 + 31) / 32;
     const int64_t id = (int64_t)blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5), window = id / n_chunks;
     const bool is_v = blockIdx.y != 0;
     const int chunk = (int)(id - window * n_chunks);
-    if (window * p.window >= p.n_tokens) return;
+    if (window * p.window >= p.n_tokens) { if constexpr (!WRITE) pdl_wait(); return; }
     const int first = (int)window * p.window, end = (int)min((int64_t)first + p.window, (int64_t)p.n_tokens);
     const Side& s = p.side[is_v];
     auto run = [&](auto bits) {
@@ -506,7 +513,7 @@ static int launch_values(Params& p, int n_sm, cudaStream_t st)
 {
     const int64_t n_chunks = (p.H * p.nu * 4 + 31) / 32;
     auto windows = [&]() { return ((int64_t)p.n_tokens + p.window - 1) / p.window; };
-    p.window = 32;
+    p.window = MAX_WINDOW;
     while (p.window > 1 && windows() * n_chunks * 2 < (int64_t)n_sm * WARPS_PER_SM) p.window /= 2;
     const int64_t blocks = (windows() * n_chunks + THREADS / 32 - 1) / (THREADS / 32);
     if (blocks > INT_MAX) return RPTQ_ERR_UNSUPPORTED;
