@@ -306,13 +306,12 @@ class KvCache:
 
     def pools(self, k_pages, v_pages):
         """(pointer, pointer, pages) of the two pools."""
-        for t, b in ((k_pages, self.k_page_bytes), (v_pages, self.v_page_bytes)):
-            shape = t.shape
-            if t.dtype is not _torch.uint8 or len(shape) != 2 or shape[1] != b or not t.is_contiguous() or t.get_device() != self.device:
-                raise ValueError(f"a pool is a contiguous uint8 [n_pages][{b}] on the cache's device, got {t.dtype} {tuple(shape)}")
-        if k_pages.shape[0] != v_pages.shape[0]:
-            raise ValueError("the pools of keys and values have different numbers of pages")
-        return k_pages.data_ptr(), v_pages.data_ptr(), k_pages.shape[0]
+        n = k_pages.shape[0]
+        if (k_pages.shape == (n, self.k_page_bytes) and v_pages.shape == (n, self.v_page_bytes) and k_pages.dtype is _torch.uint8 and v_pages.dtype is _torch.uint8
+                and k_pages.get_device() == self.device == v_pages.get_device() and k_pages.is_contiguous() and v_pages.is_contiguous()):
+            return k_pages.data_ptr(), v_pages.data_ptr(), n
+        raise ValueError(f"the pools are contiguous uint8 tensors [n_pages][{self.k_page_bytes}] and [n_pages][{self.v_page_bytes}] on the cache's device, got "
+                         f"{k_pages.dtype} {tuple(k_pages.shape)} and {v_pages.dtype} {tuple(v_pages.shape)}")
 
     def destroy(self) -> None:
         if getattr(self, "_h", None) is not None:

@@ -9,7 +9,7 @@ namespace rptq {
 namespace attn_paged {
 
 constexpr int MAX_KEYS = 1 << 30;              // per sequence
-constexpr int MIN_SHARE = PAIR_COST + 4;       // least share of a group
+constexpr int MIN_SHARE = PAIR_COST + 2;       // least share of a group
 constexpr int WHOLE_TILES = 4;                 // pairs of at most so many tiles are not split
 
 // How a cache is worked on with G query heads per cached head: the instance knows its sizes (`exact`), warps of a group, blocks per SM.
