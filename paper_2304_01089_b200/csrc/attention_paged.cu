@@ -21,7 +21,7 @@ static Plan plan_of(const rptq_kv_cache_t* c, int G)
     x.un = x.exact ? c->nu : c->nu <= 4 ? 4 : 8;
     x.warps = G <= WARP_Q ? 1 : G <= 2 * WARP_Q ? 2 : 4;
     x.chunks = (G + x.warps * WARP_Q - 1) / (x.warps * WARP_Q);
-    x.smem = WARPS / x.warps * STAGES * stage_bytes(c->k.bits, c->v.bits, c->nu) + WARPS * scratch_bytes(x.un);
+    x.smem = WARPS / x.warps * STAGES * stage_bytes(c->k.bits, c->v.bits, c->nu) + WARPS * scratch_bytes(c->k.bits, x.un);
     const int by_smem = (SMEM_MAX + 1024) / (x.smem + 1024);
     x.blocks_per_sm = by_smem < BLOCKS_PER_SM ? by_smem : BLOCKS_PER_SM;
     return x;

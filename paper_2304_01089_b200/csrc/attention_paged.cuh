@@ -17,8 +17,8 @@
 //     scores of a row alike). The query becomes integers of 31 bits with one exponent per head, four signed bytes in four
 //     columns of mma.sync m16n8k32 (u8 codes x s8 bytes, exact): two query heads fill the eight columns. Of 4-bit codes the packed word itself
 //     is an operand: its bytes are 16 hi + lo, so with the integer y of hi's channel counted in units 16 times larger and x - y in place
-//     of lo's x, x lo + 16 y hi = (x - y) lo + y (16 hi + lo) takes one AND for eight codes. A channel's query is off by at most 2^-27
-//     of the head's largest: less than 32-bit sums lose;
+//     of lo's x, x lo + 16 y hi = (x - y) lo + y (16 hi + lo) takes one AND for eight codes; 3-bit pages are made for the same (kv_pages.cuh). A
+//     channel's query is off by at most 2^-27 of the head's largest (3 bits: 2^-25): no more than 32-bit sums lose;
 //   - probabilities as unsigned 32-bit integers, four bytes in four columns, V^T as operand A. The sums are exact, and keys behind the last
 //     one or on a page that does not exist have P = 0 whatever bytes lie there. (Codes as fp16 with eight query heads in a warp's eight
 //     columns took three instructions per four codes to convert, twice the registers, and 50 us where this takes 24 us: 64 sequences of
@@ -49,7 +49,6 @@ constexpr int WARP_Q = 2;                      // query heads of a warp
 constexpr float HEAD = 4.0f;                   // how far above the largest score a moved reference lies, in powers of two
 constexpr float NO_REF = -1.0e30f;
 constexpr int FLUSH_TILES = 1000;              // 32 keys x 255 x 255 a tile stay below 2^31 in 32-bit sums for 1032 tiles
-constexpr int UNIT_PITCH = 36;                 // words between the units of the staged query: the four pieces of a row group in different banks
 
 constexpr int SMEM_MAX = 227 * 1024;           // of a block
 constexpr int STAGES = 3;                      // of a group's ring (four: 3 % slower at 4 bits, one long sequence; five: 8 % slower with several)
@@ -57,7 +56,9 @@ constexpr int BLOCKS_PER_SM = 3;               // by registers: 168 a thread
 // bytes of a stage of a ring: two slabs of each tensor
 __host__ __device__ constexpr int stage_bytes(int bits_k, int bits_v, int nu) { return 2 * SLAB * 4 * nu * (bits_k + bits_v); }
 // a warp's own: the staged query of one head, or the tile's probabilities
-__host__ __device__ constexpr int scratch_bytes(int un) { return un * UNIT_PITCH * 4 > WARP_Q * TILE * 4 ? un * UNIT_PITCH * 4 : WARP_Q * TILE * 4; }
+__host__ __device__ constexpr int unit_pitch(int bits_k) { return bits_k == 3 ? 44 : 36; }       // words between the units of the staged query: the
+                                                                 // four pieces of a row group in different banks
+__host__ __device__ constexpr int scratch_bytes(int bits_k, int un) { return un * unit_pitch(bits_k) * 4 > WARP_Q * TILE * 4 ? un * unit_pitch(bits_k) * 4 : WARP_Q * TILE * 4; }
 __host__ __device__ constexpr int part_pitch(int nu) { return 4 + 32 * nu; }
 struct Params {
     const uint8_t *k, *v;
@@ -208,9 +209,10 @@ template <int BK, int BV, int UN, bool EXACT, int R>
 __global__ void __launch_bounds__(THREADS, BLOCKS_PER_SM)
 paged_kernel(const Params p)
 {
-    constexpr int KQ = BK == 8 ? (UN + 1) / 2 : (UN + 3) / 4, KI = BK == 8 ? 2 : 4;      // groups of four 16-byte pieces, products per group
-    constexpr int NB = BV != 3 ? (UN + 1) / 2 : UN <= 4 ? 2 : 4;                         // blocks of four products of 16 channels
-    constexpr float HI = BV == 8 ? 1.0f : 0.0625f;         // channels of the upper nibbles count 16 n
+    constexpr int KQ = BK == 8 ? (UN + 1) / 2 : (UN + 3) / 4, KI = BK == 8 ? 2 : BK == 4 ? 4 : 5;      // groups of four 16-byte pieces, products per group
+    // A lane's channels of the outputs: NB runs of eight (8 bits: of twice four; 3 bits: a half of a unit is two runs), and the products they take
+    constexpr int NB = BV != 3 ? (UN + 1) / 2 : UN <= 4 ? 2 : 4, NM = BV == 3 ? 5 * NB : 4 * NB;
+    constexpr float HI = BV == 4 ? 0.0625f : 1.0f;         // 4 bits: channels of the upper nibbles count 16 n
     constexpr bool RAW = BV == 4;                          // their rows hold 16 hi + lo
     extern __shared__ __align__(16) uint8_t smem[];
 
@@ -221,7 +223,7 @@ paged_kernel(const Params p)
     const int group = warp_in_block / warps, warp = warp_in_block - group * warps;
     const int64_t n_groups = (int64_t)gridDim.x * (WARPS / warps), me = (int64_t)group * gridDim.x + blockIdx.x;
     uint8_t* ring = smem + group * STAGES * stage;
-    uint32_t* scratch = reinterpret_cast<uint32_t*>(smem + (WARPS / warps) * STAGES * stage + warp_in_block * scratch_bytes(UN));
+    uint32_t* scratch = reinterpret_cast<uint32_t*>(smem + (WARPS / warps) * STAGES * stage + warp_in_block * scratch_bytes(BK, UN));
     const int pairs = p.H * p.chunks, slabs_per_page = p.P / SLAB;
     auto sync_group = [&]() {
         if (R == 4) __syncthreads();
@@ -325,7 +327,7 @@ paged_kernel(const Params p)
     // ---- per pair
     uint32_t qb[KQ * KI][2];
     float coef = 0.f, ref = NO_REF;                        // of query head t4 >> 1
-    int O[NB][4][4], L[4];
+    int O[NM][4], L[4];
     float F[NB][4][2], Fl = 0.f;                           // sums that were taken out of the integers; my two of the four digits
     int since = 0, n_heads = 0;
     const float weight = (t4 & 1) ? 65536.0f : 1.0f;       // of my two digits d0 + 2^8 d1
@@ -365,17 +367,61 @@ paged_kernel(const Params p)
             const int e = max((int)(top >> 23), 30);                       // |x| < 2^(e - 126): |x| 2^(156 - e) < 2^30
             const float f = finite ? __int_as_float((283 - e) << 23) : 0.f;
             if ((t4 >> 1) == q) coef = finite ? __int_as_float((e - 29) << 23) * p.scale_log2e : __int_as_float(0x7FC00000);
+            // signed bytes d with X = d0 + 2^8 d1 + 2^16 d2 + 2^24 d3
+            auto digits = [](int X) { return ((uint32_t)X + 0x00808080u) ^ 0x00808080u; };
+            constexpr int PITCH = unit_pitch(BK);
             __syncwarp();
+            if constexpr (BK == 3) {
+                // A product has c0, c0 + 8 c1, c0 + 8 c1 + 64 b, .. as factors: the query's integers of c0, c1 / 8, b / 64 (of the single bits on top,
+                // worth 4: / 16 and / 32), each less the next. First the integers, channel by channel and those of the single bits behind them
+                const int in_half = lane & 15;
+                const float g = f * (in_half >= 12 ? 0.015625f : (in_half >= 4 && in_half < 8) || in_half >= 10 ? 0.125f : 1.0f);
 #pragma unroll
-            for (int i = 0; i < UN; ++i) {
-                // channels whose codes are upper nibbles are multiplied by 16 n (3 bits) or, of 4 bits, by the whole byte
-                int X = __float2int_rn(x[q][i] * (BK != 8 && (lane & 4) ? f * 0.0625f : f));
-                if constexpr (BK == 4) {
-                    const int y = __shfl_xor_sync(0xffffffffu, X, 4);
-                    if (!(lane & 4)) X -= y;
+                for (int i = 0; i < UN; ++i) {
+                    if (i >= nu) break;
+                    scratch[i * PITCH + lane] = (uint32_t)__float2int_rn(x[q][i] * g);
+                    if (in_half >= 12) scratch[i * PITCH + 32 + 4 * (lane >> 4) + (lane & 3)] = (uint32_t)__float2int_rn(x[q][i] * (f * (lane & 1 ? 0.03125f : 0.0625f)));
                 }
-                // signed bytes d with X = d0 + 2^8 d1 + 2^16 d2 + 2^24 d3
-                if (i < nu) scratch[i * UNIT_PITCH + lane] = ((uint32_t)X + 0x00808080u) ^ 0x00808080u;
+                __syncwarp();
+                // then the 10 operands' four bytes each
+                uint32_t z[UN][2];
+                auto entry = [&](const uint32_t* y, int e) {
+                    const int op = e >> 2, i = e & 3;
+                    int a, b;                                                  // b < 0: nothing is taken off
+                    if (op < 6) {
+                        const int h = op >= 3 ? 16 : 0, of = op >= 3 ? op - 3 : op;
+                        a = h + (of == 2 ? 12 : 4 * of) + i;
+                        b = of == 2 ? -1 : h + (of == 1 ? 12 : 4) + i;
+                    } else {
+                        const int h = 16 * (i >> 1), bit = 32 + 4 * (i >> 1) + 2 * (i & 1);
+                        a = op == 6 ? h + 8 + (i & 1) : op == 7 ? h + 10 + (i & 1) : op == 8 ? bit : bit + 1;
+                        b = op == 6 ? h + 10 + (i & 1) : op == 7 ? bit : op == 8 ? bit + 1 : -1;
+                    }
+                    return digits((int)y[a] - (b < 0 ? 0 : (int)y[b]));
+                };
+#pragma unroll
+                for (int i = 0; i < UN; ++i) {
+                    const uint32_t* y = scratch + min(i, nu - 1) * PITCH;
+                    z[i][0] = entry(y, lane);
+                    z[i][1] = entry(y, 32 + (lane & 7));
+                }
+                __syncwarp();
+#pragma unroll
+                for (int i = 0; i < UN; ++i) {
+                    if (i >= nu) break;
+                    scratch[i * PITCH + lane] = z[i][0];
+                    if (lane < 8) scratch[i * PITCH + 32 + lane] = z[i][1];
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < UN; ++i) {
+                    int X = __float2int_rn(x[q][i] * (BK == 4 && (lane & 4) ? f * 0.0625f : f));
+                    if constexpr (BK == 4) {                                   // channels whose codes are upper nibbles are multiplied by the whole byte
+                        const int y = __shfl_xor_sync(0xffffffffu, X, 4);
+                        if (!(lane & 4)) X -= y;
+                    }
+                    if (i < nu) scratch[i * PITCH + lane] = digits(X);
+                }
             }
             __syncwarp();
 #pragma unroll
@@ -384,7 +430,7 @@ paged_kernel(const Params p)
                 for (int i = 0; i < KI; ++i) {
                     const int unit = BK == 8 ? 2 * j + (t4 >> 1) : 4 * j + t4, at = BK == 8 ? 16 * (t4 & 1) + 8 * i : 8 * i;
                     if (unit < nu && (g8 >> 2) == q) {
-                        const uint4* z = reinterpret_cast<const uint4*>(scratch + unit * UNIT_PITCH + at);
+                        const uint4* z = reinterpret_cast<const uint4*>(scratch + unit * PITCH + at);
                         const uint4 a = z[0], b = z[1];
                         qb[j * KI + i][0] = __byte_perm(__byte_perm(a.x, a.y, limb_sel), __byte_perm(a.z, a.w, limb_sel), 0x5410);
                         qb[j * KI + i][1] = __byte_perm(__byte_perm(b.x, b.y, limb_sel), __byte_perm(b.z, b.w, limb_sel), 0x5410);
@@ -394,13 +440,13 @@ paged_kernel(const Params p)
         __syncwarp();
         ref = NO_REF;
 #pragma unroll
+        for (int m = 0; m < NM; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) O[m][i] = 0;
+#pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) O[b][e][i] = 0;
-                F[b][e][0] = F[b][e][1] = 0.f;
-            }
+            for (int e = 0; e < 4; ++e) F[b][e][0] = F[b][e][1] = 0.f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) L[i] = 0;
         Fl = 0.f;
@@ -409,18 +455,48 @@ paged_kernel(const Params p)
     // The integers move into the 32-bit floating sums, times f. The two digits are joined in floating point: a sum may have 31 bits.
     auto flush = [&](float f) {
         const float w0 = weight, w1 = 256.0f * weight;
+        if constexpr (BV == 3) {
+            // operand k of a half of a unit is row k & 1 of product k >> 1: of A byte e c0, c0 + 8 c1, all of it; of C byte i c0, c0 + 8 c1, and the
+            // single bits on top
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
+            for (int j = 0; j < NB / 2; ++j) {
+                int v[2][16];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                int (&o)[4] = O[b][e];
-                if constexpr (RAW) { o[2] -= o[0]; o[3] -= o[1]; }
+                for (int d = 0; d < 2; ++d) {
+                    auto sum = [&](int k) { return O[10 * j + (k >> 1)][2 * (k & 1) + d]; };
 #pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    F[b][e][r] = f * (F[b][e][r] + __fmaf_rn(w1, (float)o[2 * r + 1], w0 * (float)o[2 * r]));
-                    o[2 * r] = o[2 * r + 1] = 0;
+                    for (int e = 0; e < 4; ++e) {
+                        v[d][e] = sum(3 * e);
+                        v[d][4 + e] = (sum(3 * e + 1) - sum(3 * e)) >> 3;
+                        v[d][12 + e] = (sum(3 * e + 2) - sum(3 * e + 1)) >> 6;
+                    }
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        v[d][8 + i] = sum(12 + 4 * i);
+                        v[d][10 + i] = (sum(13 + 4 * i) - sum(12 + 4 * i)) >> 3;
+                        v[d][12 + 2 * i] += ((sum(14 + 4 * i) - sum(13 + 4 * i)) >> 6) * 4;
+                        v[d][13 + 2 * i] += ((sum(15 + 4 * i) - sum(14 + 4 * i)) >> 7) * 4;
+                    }
+                }
+#pragma unroll
+                for (int n = 0; n < 16; ++n) {
+                    float& x = F[2 * j + (n >> 3)][n & 3][(n >> 2) & 1];
+                    x = f * (x + __fmaf_rn(w1, (float)v[1][n], w0 * (float)v[0][n]));
                 }
             }
+        } else {
+#pragma unroll
+            for (int m = 0; m < NM; ++m) {
+                int (&o)[4] = O[m];
+                if constexpr (RAW) { o[2] -= o[0]; o[3] -= o[1]; }
+#pragma unroll
+                for (int r = 0; r < 2; ++r) F[m >> 2][m & 3][r] = f * (F[m >> 2][m & 3][r] + __fmaf_rn(w1, (float)o[2 * r + 1], w0 * (float)o[2 * r]));
+            }
+        }
+#pragma unroll
+        for (int m = 0; m < NM; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) O[m][i] = 0;
         Fl = f * (Fl + __fmaf_rn(w1, (float)L[1], w0 * (float)L[0]));
 #pragma unroll
         for (int i = 0; i < 4; ++i) L[i] = 0;
@@ -444,17 +520,19 @@ paged_kernel(const Params p)
                 const int n = min(pieces, 4), piece = min(t4, n - 1);
                 if constexpr (BK == 3) {
                     const uint8_t* a = base + SLAB * 48 * j + (n * g8 + piece) * 4;
-                    uint32_t x[4], y[4];
+                    uint32_t x[3], y[3];
 #pragma unroll
                     for (int i = 0; i < 3; ++i) {
                         x[i] = *reinterpret_cast<const uint32_t*>(a + SLAB * 4 * n * i);
                         y[i] = *reinterpret_cast<const uint32_t*>(a + SLAB * 4 * n * i + 32 * n);
                     }
-                    x[3] = ((x[0] >> 3) & 0x11111111u) | ((x[1] >> 2) & 0x22222222u) | ((x[2] >> 1) & 0x44444444u);
-                    y[3] = ((y[0] >> 3) & 0x11111111u) | ((y[1] >> 2) & 0x22222222u) | ((y[2] >> 1) & 0x44444444u);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        mma_u8s8(acc, x[i] & 0x07070707u, y[i] & 0x07070707u, x[i] & 0x70707070u, y[i] & 0x70707070u, qb[4 * j + i][0], qb[4 * j + i][1]);
+                    constexpr uint32_t M7 = 0x07070707u, M3F = 0x3F3F3F3Fu, M7F = 0x7F7F7F7Fu;
+                    const uint32_t (*b)[2] = qb + 5 * j;
+                    mma_u8s8(acc, x[0] & M7, y[0] & M7, x[0] & M3F, y[0] & M3F, b[0][0], b[0][1]);
+                    mma_u8s8(acc, x[0], y[0], x[1] & M7, y[1] & M7, b[1][0], b[1][1]);
+                    mma_u8s8(acc, x[1] & M3F, y[1] & M3F, x[1], y[1], b[2][0], b[2][1]);
+                    mma_u8s8(acc, x[2] & M7, y[2] & M7, x[2] & M3F, y[2] & M3F, b[3][0], b[3][1]);
+                    mma_u8s8(acc, x[2] & M7F, y[2] & M7F, x[2], y[2], b[4][0], b[4][1]);
                 } else {
                     const uint8_t* a = base + SLAB * 64 * j + (n * g8 + piece) * 16;
                     const uint4 xa = *reinterpret_cast<const uint4*>(a), ya = *reinterpret_cast<const uint4*>(a + 128 * n);
@@ -511,8 +589,8 @@ paged_kernel(const Params p)
                 if (!EXACT && x >= nu) break;
                 const uint8_t* at = vs + 64 * (8 * x + g8) + 16 * t4;
                 const uint4 m = *reinterpret_cast<const uint4*>(at), n = *reinterpret_cast<const uint4*>(at + v_slab);
-                mma_u8(O[x >> 1][2 * (x & 1)], m.x, m.y, n.x, n.y, pb[0], pb[1]);
-                mma_u8(O[x >> 1][2 * (x & 1) + 1], m.z, m.w, n.z, n.w, pb[0], pb[1]);
+                mma_u8(O[2 * x], m.x, m.y, n.x, n.y, pb[0], pb[1]);
+                mma_u8(O[2 * x + 1], m.z, m.w, n.z, n.w, pb[0], pb[1]);
             }
         } else if constexpr (BV == 4) {
 #pragma unroll
@@ -520,37 +598,32 @@ paged_kernel(const Params p)
                 if (!EXACT && 2 * b >= nu) break;
                 const int group = 8 * (b + 1) <= 4 * (EXACT ? UN : 0) ? 8 * b + g8 : min(8 * b + g8, 4 * nu - 1);
                 const uint4 x = *reinterpret_cast<const uint4*>(vs + 64 * group + 16 * t4), y = *reinterpret_cast<const uint4*>(vs + v_slab + 64 * group + 16 * t4);
-                mma_u8(O[b][0], x.x & 0x0F0F0F0Fu, x.x, y.x & 0x0F0F0F0Fu, y.x, pb[0], pb[1]);
-                mma_u8(O[b][1], x.y & 0x0F0F0F0Fu, x.y, y.y & 0x0F0F0F0Fu, y.y, pb[0], pb[1]);
-                mma_u8(O[b][2], x.z & 0x0F0F0F0Fu, x.z, y.z & 0x0F0F0F0Fu, y.z, pb[0], pb[1]);
-                mma_u8(O[b][3], x.w & 0x0F0F0F0Fu, x.w, y.w & 0x0F0F0F0Fu, y.w, pb[0], pb[1]);
+                mma_u8(O[4 * b + 0], x.x & 0x0F0F0F0Fu, x.x, y.x & 0x0F0F0F0Fu, y.x, pb[0], pb[1]);
+                mma_u8(O[4 * b + 1], x.y & 0x0F0F0F0Fu, x.y, y.y & 0x0F0F0F0Fu, y.y, pb[0], pb[1]);
+                mma_u8(O[4 * b + 2], x.z & 0x0F0F0F0Fu, x.z, y.z & 0x0F0F0F0Fu, y.z, pb[0], pb[1]);
+                mma_u8(O[4 * b + 3], x.w & 0x0F0F0F0Fu, x.w, y.w & 0x0F0F0F0Fu, y.w, pb[0], pb[1]);
             }
         } else {
-            // up to four units: two row groups share a unit, two of its four words of eight channels each; the fourth word is in the others' top bits
-            const int unit = min(UN <= 4 ? g8 >> 1 : g8, nu - 1);
-            uint32_t w[2][3][4];
+            // a row group has a half of a unit: four words of A and two of C
+            constexpr uint32_t M7 = 0x07070707u, M3F = 0x3F3F3F3Fu, M7F = 0x7F7F7F7Fu;
 #pragma unroll
-            for (int half = 0; half < 2; ++half)
-#pragma unroll
-                for (int i = 0; i < 3; ++i) {
-                    const uint4 x = *reinterpret_cast<const uint4*>(vs + half * v_slab + 64 * (3 * unit + i) + 16 * t4);
-                    w[half][i][0] = x.x; w[half][i][1] = x.y; w[half][i][2] = x.z; w[half][i][3] = x.w;
-                }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                uint32_t u[4][2];
+            for (int j = 0; j < NB / 2; ++j) {
+                const int unit = min(4 * j + (g8 >> 1), nu - 1);
+                const uint8_t* at = vs + 64 * (3 * unit) + 16 * t4;
+                uint32_t w[2][6];
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
-                    const uint32_t x = w[half][0][e], y = w[half][1][e], z = w[half][2][e];
-                    const uint32_t tail = ((x >> 3) & 0x11111111u) | ((y >> 2) & 0x22222222u) | ((z >> 1) & 0x44444444u);
-                    u[0][half] = UN <= 4 && (g8 & 1) ? z : x;
-                    u[1][half] = UN <= 4 && (g8 & 1) ? tail : y;
-                    u[2][half] = z;
-                    u[3][half] = tail;
+                    const uint4 a = *reinterpret_cast<const uint4*>(at + half * v_slab + 64 * (g8 & 1));
+                    const uint2 c = *reinterpret_cast<const uint2*>(at + half * v_slab + 128 + 8 * (g8 & 1));
+                    w[half][0] = a.x; w[half][1] = a.y; w[half][2] = a.z; w[half][3] = a.w; w[half][4] = c.x; w[half][5] = c.y;
                 }
+                auto op = [&](int half, int k) -> uint32_t {                   // operand k of 20
+                    if (k < 12) return k % 3 == 0 ? w[half][k / 3] & M7 : k % 3 == 1 ? w[half][k / 3] & M3F : w[half][k / 3];
+                    const uint32_t c = w[half][4 + (k - 12) / 4];
+                    return k % 4 == 0 ? c & M7 : k % 4 == 1 ? c & M3F : k % 4 == 2 ? c & M7F : c;
+                };
 #pragma unroll
-                for (int b = 0; b < NB; ++b)
-                    mma_u8(O[b][e], u[b][0] & 0x07070707u, u[b][0] & 0x70707070u, u[b][1] & 0x07070707u, u[b][1] & 0x70707070u, pb[0], pb[1]);
+                for (int m = 0; m < 10; ++m) mma_u8(O[10 * j + m], op(0, 2 * m), op(0, 2 * m + 1), op(1, 2 * m), op(1, 2 * m + 1), pb[0], pb[1]);
             }
         }
         __syncwarp();                                          // the scratch may be written again (one warp: and the stage)
@@ -586,7 +659,7 @@ paged_kernel(const Params p)
             constexpr int N = BV == 8 ? 4 : 8;
 #pragma unroll
             for (int x = 0; x < 8 / N; ++x) {
-                const int ch = BV == 8 ? 4 * (8 * (2 * b + x) + g8) : BV == 4 ? 8 * (8 * b + g8) : UN <= 4 ? 32 * (g8 >> 1) + 16 * (g8 & 1) + 8 * b : 32 * g8 + 8 * b;
+                const int ch = BV == 8 ? 4 * (8 * (2 * b + x) + g8) : BV == 4 ? 8 * (8 * b + g8) : 32 * (4 * (b >> 1) + (g8 >> 1)) + 16 * (g8 & 1) + 8 * (b & 1);
                 if (!mine || ch >= 32 * nu) continue;
                 float y[N];
 #pragma unroll

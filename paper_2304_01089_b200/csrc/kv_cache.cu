@@ -196,9 +196,9 @@ __device__ __forceinline__ void write_rows(const Params& p, const Side& s, int f
         const float4 x = par[i];
         inv[i] = make_float2(x.x, x.z); zc[2 * i] = __float_as_int(x.y); zc[2 * i + 1] = __float_as_int(x.w);
     }
-    constexpr int WORDS = BITS == 8 ? 2 : 1;               // a lane's (3 bits: of the first three lanes of a unit)
+    constexpr int WORDS = BITS == 8 ? 2 : 1;               // a lane's (3 bits: the unit's first and third lane have A, the second has C)
     const bool writes = at.valid && (BITS == 3 ? at.w < 3 : at.real > 0);
-    const int word = BITS == 8 ? 2 * at.w : at.w;
+    const int word = BITS == 8 ? 2 * at.w : BITS == 4 ? at.w : (3 - at.w) % 3;
     // my first word of key 0 of the head's first slab, and the bytes between keys
     uint8_t* const mine = s.pages + slab_offset(0, 0, at.h, p.P / SLAB, 0, s.slab_bytes) + (V ? v_byte<BITS>(at.u, writes ? word : 0, 0, 0) : k_word<BITS>(p.nu, at.u, writes ? word : 0, 0));
     const int key_step = V ? 0 : k_word<BITS>(p.nu, at.u, 0, 1) - k_word<BITS>(p.nu, at.u, 0, 0);
@@ -225,8 +225,11 @@ __device__ __forceinline__ void write_rows(const Params& p, const Side& s, int f
             } else if constexpr (BITS == 4) {
                 w[0][k] = sat_nibble_word(v);
             } else {
-                const uint32_t x7 = sat_nibble_word_max7(v), tail = __shfl_sync(0xffffffffu, x7, lane | 3);
-                w[0][k] = x7 | (((tail >> at.w) & 0x11111111u) << 3);
+                // code i in the low nibble of byte i, code 4 + i in the high one; odd lanes have codes 8 .. 15 of the half
+                const uint32_t x = sat_nibble_word_max7(v), beside = __shfl_xor_sync(0xffffffffu, x, 1);
+                const uint32_t c = (x & 0x0747u) | ((x >> 13) & 0x3838u) | ((x >> 7) & 0x80u) | ((x >> 8) & 0x4000u) | ((x >> 15) & 0x8000u);
+                const uint32_t other = __shfl_xor_sync(0xffffffffu, c, 2);
+                w[0][k] = at.w & 1 ? c | (other << 16) : (x & 0x07070707u) | ((x >> 1) & 0x38383838u) | ((beside << 2) & 0xC0C0C0C0u);
             }
         }
         if (!writes) return;
@@ -293,7 +296,7 @@ __device__ __forceinline__ void read_rows(const Params& p, const Side& s, int fi
     pdl_wait();                                            // (the handle's tables were there before any launch)
     constexpr int WORDS = BITS == 8 ? 2 : 1;
     const bool reads = at.valid && (BITS == 3 ? at.w < 3 : at.real > 0);
-    const int word = BITS == 8 ? 2 * at.w : at.w;
+    const int word = BITS == 8 ? 2 * at.w : BITS == 4 ? at.w : (3 - at.w) % 3;
     const uint8_t* const mine = s.pages + slab_offset(0, 0, at.h, p.P / SLAB, 0, s.slab_bytes) + (V ? v_byte<BITS>(at.u, reads ? word : 0, 0, 0) : k_word<BITS>(p.nu, at.u, reads ? word : 0, 0));
     const int key_step = V ? 0 : k_word<BITS>(p.nu, at.u, 0, 1) - k_word<BITS>(p.nu, at.u, 0, 0);
     T* const row0 = static_cast<T*>(s.rows) + (int64_t)first * s.ld + at.h * p.d + at.ch;
@@ -345,15 +348,18 @@ __device__ __forceinline__ void read_rows(const Params& p, const Side& s, int fi
             uint32_t q[2];                                 // codes as bytes
             if constexpr (BITS == 8) {
                 q[0] = words.w[0][k]; q[1] = words.w[1][k];
-            } else {
-                uint32_t x = words.w[0][k];
-                if constexpr (BITS == 3) {
-                    uint32_t tail = 0u;
-#pragma unroll
-                    for (int j = 0; j < 3; ++j) tail |= ((__shfl_sync(0xffffffffu, x, (lane & ~3) + j) >> 3) & 0x11111111u) << j;
-                    x = at.w == 3 ? tail : x & 0x77777777u;
-                }
+            } else if constexpr (BITS == 4) {
+                const uint32_t x = words.w[0][k];
                 q[0] = x & 0x0F0F0F0Fu; q[1] = (x >> 4) & 0x0F0F0F0Fu;
+            } else {
+                const uint32_t x = words.w[0][k], a = __shfl_sync(0xffffffffu, x, lane & ~1);
+                const uint32_t c = __shfl_sync(0xffffffffu, x, (lane & ~3) + 1) >> (at.w == 3 ? 16 : 0);      // (its low half)
+                if (at.w & 1) {
+                    q[0] = (c & 0x0707u) | (((c >> 3) & 0x0707u) << 16);
+                    q[1] = ((a >> 6) & 0x03030303u) | ((c >> 4) & 0x4u) | ((c << 3) & 0x400u) | ((c << 4) & 0x40000u) | ((c << 11) & 0x4000000u);
+                } else {
+                    q[0] = a & 0x07070707u; q[1] = (a >> 3) & 0x07070707u;
+                }
             }
             float2 y[4];
 #pragma unroll
@@ -453,7 +459,8 @@ __device__ void write_code_rows(const Params& p, const Side& s, bool is_v)
         const uint8_t* row = static_cast<const uint8_t*>(s.rows) + (int64_t)token * s.ld;
 #pragma unroll
         for (int c = 0; c < 32; ++c) q[c] = c < real ? row_code<BITS>(row, s.pos[ch0 + c]) : 0u;
-        pack32<BITS>(q, w);
+        if constexpr (BITS == 3) pack_three(q, w);
+        else pack32<BITS>(q, w);
         store_unit<BITS>(s.pages + slab_offset(page, s.page_bytes, h, p.P / SLAB, key / SLAB, s.slab_bytes), is_v, p.nu, u, key % SLAB, w);
     }
 }
@@ -478,8 +485,7 @@ __device__ void read_code_rows(const Params& p, const Side& s, bool is_v)
             auto byte = [&](int word) -> uint32_t { return is_v ? slab[v_byte<BITS>(u, word, b, r)] : slab[k_word<BITS>(p.nu, u, word, r) + b]; };
             if constexpr (BITS == 8) q[c] = byte(at >> 2);
             else if constexpr (BITS == 4) q[c] = (byte(at >> 3) >> sh) & 15u;
-            else if (at < 24) q[c] = (byte(at >> 3) >> sh) & 7u;
-            else q[c] = ((byte(0) >> (sh + 3)) & 1u) | (((byte(1) >> (sh + 3)) & 1u) << 1) | (((byte(2) >> (sh + 3)) & 1u) << 2);
+            else q[c] = code_of_three([&](int w, int e) -> uint32_t { return is_v ? slab[v_byte<BITS>(u, w, e, r)] : slab[k_word<BITS>(p.nu, u, w, r) + e]; }, at);
         }
         pack32<BITS>(q, w);
         uint32_t* out = reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(s.rows) + (int64_t)token * s.ld) + (int64_t)unit * BITS;
