@@ -453,7 +453,7 @@ int rptq_kv_cache_read(const rptq_kv_cache_t* cache, const void* k_pages, const 
  *               nothing is kept in it between calls. Calls that may overlap on the GPU need a workspace each
  * An entry outside 0 .. n_pages - 1 records RPTQ_ERR_BAD_SLOT in the status word and its keys are left out. What the slots behind a
  * sequence's last key hold does not matter. A query that is not finite gives NaN. n_seq, n_q_heads <= 65535,
- * table_width * page_size <= 2^30.
+ * table_width * page_size <= 2^30; n_seq * n_q_heads * (table_width * page_size / 32 + 5) < 2^30.
  */
 int64_t rptq_attention_paged_workspace_bytes(const rptq_kv_cache_t* cache, int n_q_heads);
 int rptq_attention_paged(const rptq_kv_cache_t* cache, const void* q, int64_t ldq, int q_type, int n_q_heads, int n_seq,

@@ -63,6 +63,10 @@ int rptq_attention_paged(const rptq_kv_cache_t* cache, const void* q, int64_t ld
     if (ldq < Cq || ldo < Cq) return RPTQ_ERR_INVALID_ARG;
     if (!aligned16(k_pages) || !aligned16(v_pages)) return RPTQ_ERR_INVALID_ARG;
     if ((int64_t)table_width * cache->P > MAX_KEYS || n_seq > 65535 || n_q_heads > 65535) return RPTQ_ERR_UNSUPPORTED;
+    const Plan x = plan_of(cache, n_q_heads / cache->H);
+    // what the longest sequences could need, in tiles: places in the list are 32 bits, groups' shares of it included
+    const int64_t max_tiles = ((int64_t)table_width * cache->P + TILE - 1) / TILE, all_pairs = (int64_t)n_seq * cache->H * x.chunks;
+    if (all_pairs * (max_tiles + PAIR_COST) > INT_MAX / 2) return RPTQ_ERR_UNSUPPORTED;
     if (n_seq == 0) return RPTQ_OK;
     if (!k_pages || !v_pages || !q || !out || !seq_lens || !workspace || (table_width > 0 && !page_table)) return RPTQ_ERR_INVALID_ARG;
     if (((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out)) & 1u) || !aligned16(workspace)) return RPTQ_ERR_INVALID_ARG;
@@ -83,7 +87,6 @@ int rptq_attention_paged(const rptq_kv_cache_t* cache, const void* q, int64_t ld
     p.table = page_table; p.ld_table = ld_table; p.lens = seq_lens;
     p.n_seq = n_seq; p.H = cache->H; p.G = n_q_heads / cache->H; p.d = cache->d; p.nu = cache->nu; p.P = cache->P;
     p.max_len = table_width * cache->P;
-    const Plan x = plan_of(cache, p.G);
     p.chunks = x.chunks;
     p.scale_log2e = qk_scale * 1.4426950408889634f;
     p.arrived = static_cast<unsigned long long*>(workspace);
@@ -93,8 +96,7 @@ int rptq_attention_paged(const rptq_kv_cache_t* cache, const void* q, int64_t ld
     const int64_t most = (int64_t)n_sm * x.blocks_per_sm;
     p.parts = reinterpret_cast<float*>(p.arrived + most * WARPS);
 
-    // what the longest sequences could need; a grid that fills the GPU is the most
-    const int64_t max_tiles = (p.max_len + TILE - 1) / TILE, all_pairs = (int64_t)n_seq * p.H * p.chunks;
+    // a grid that fills the GPU is the most
     p.whole = max_tiles <= WHOLE_TILES;
     p.min_share = MIN_SHARE;
     const int64_t groups = p.whole ? all_pairs : (all_pairs * (max_tiles + PAIR_COST) + MIN_SHARE - 1) / MIN_SHARE;

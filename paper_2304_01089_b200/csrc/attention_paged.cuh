@@ -51,8 +51,8 @@ constexpr float NO_REF = -1.0e30f;
 constexpr int FLUSH_TILES = 1000;              // 32 keys x 255 x 255 a tile stay below 2^31 in 32-bit sums for 1032 tiles
 
 constexpr int SMEM_MAX = 227 * 1024;           // of a block
-constexpr int STAGES = 3;                      // of a group's ring (four: 3 % slower at 4 bits, one long sequence; five: 8 % slower with several)
-constexpr int BLOCKS_PER_SM = 3;               // by registers: 168 a thread
+constexpr int STAGES = 2;                      // of a group's ring. (Three, more of the cache under way: 2 to 4 % slower; four: 5 %)
+constexpr int BLOCKS_PER_SM = 3;               // 168 registers a thread. (Four, 128: 4 to 17 % slower; two: up to 12 %)
 // bytes of a stage of a ring: two slabs of each tensor
 __host__ __device__ constexpr int stage_bytes(int bits_k, int bits_v, int nu) { return 2 * SLAB * 4 * nu * (bits_k + bits_v); }
 // a warp's own: the staged query of one head, or the tile's probabilities
@@ -82,48 +82,49 @@ struct Params {
 __device__ __forceinline__ int len_of(const Params& p, int s) { return min(max(p.lens[s], 0), p.max_len); }
 __device__ __forceinline__ int tiles_of(int len) { return (len + TILE - 1) / TILE; }
 
-// a / b; quotients of large numbers take ten times the instructions
-__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) { return (a | b) >> 31 ? a / b : (int64_t)((uint32_t)a / (uint32_t)b); }
-
 // Where a group is in its share: sequence, pair of the sequence (cached head and set of query heads), tiles of the pair.
 struct Cursor {
     int s, pair, t, n, nt, len;                // t: the next tile, n: how many of the pair are mine from here on, nt: all of the pair
-    int64_t begin;                             // the pair's place in the list (whole: the pair's number in the batch)
+    int begin;                                 // the pair's place in the list (whole: the pair's number in the batch)
     bool ok;
 };
 
-// All lanes: the length of the list over its pairs per sequence.
-__device__ __forceinline__ int64_t list_per_pair(const Params& p)
+// All lanes: a group's share of the list, and the list's length. Equal shares, but not less than min_share, nor so little that the
+// longest pair falls into many more parts than one warp joins in the time of its tiles: of n parts of nt tiles that takes about nt / n x 0.5 us and
+// n / 8 x 1.2 us, the least when a part has sqrt(0.3 nt). (The host sees to it that the list and its places stay below 2^31.)
+__device__ __forceinline__ int find_shares(const Params& p, int pairs, int n_groups, int& share)
 {
-    int64_t n = 0;
+    int n = 0, longest = 0;
     for (int s = threadIdx.x & 31; s < p.n_seq; s += 32) {
         const int nt = tiles_of(len_of(p, s));
         n += nt > 0 ? nt + PAIR_COST : 0;
+        longest = max(longest, nt);
     }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) n += __shfl_xor_sync(0xffffffffu, n, o);
-    return n;
+    const int total = __reduce_add_sync(0xffffffffu, n) * pairs;
+    longest = __reduce_max_sync(0xffffffffu, longest);
+    share = max(max((total + n_groups - 1) / n_groups, p.min_share), PAIR_COST + (int)sqrtf(0.3f * (float)longest));
+    return total;
 }
 // My tiles of the pair c.s, c.pair, which begins at c.begin: those at places first .. end - 1 of the list.
-__device__ __forceinline__ void cut(Cursor& c, int64_t first, int64_t end)
+__device__ __forceinline__ void cut(Cursor& c, int first, int end)
 {
-    const int64_t t0 = c.begin + PAIR_COST;
-    c.t = (int)max(first - t0, (int64_t)0);
-    c.n = (int)min(end - t0, (int64_t)c.nt) - c.t;
+    const int t0 = c.begin + PAIR_COST;
+    c.t = max(first - t0, 0);
+    c.n = min(end - t0, c.nt) - c.t;
     if (c.n <= 0) c.ok = false;                // the share ends at this pair's beginning
 }
 // All lanes: the first tiles of places first .. end - 1 of the list.
-__device__ __forceinline__ void find_tile(const Params& p, int pairs, int64_t first, int64_t end, Cursor& c)
+__device__ __forceinline__ void find_tile(const Params& p, int pairs, int first, int end, Cursor& c)
 {
     const int lane = threadIdx.x & 31;
-    const int64_t x = quotient(first, pairs);
-    int64_t before = 0;
+    const int x = first / pairs;
+    int before = 0;
     for (int s0 = 0; s0 < p.n_seq; s0 += 32) {
         const int len = s0 + lane < p.n_seq ? len_of(p, s0 + lane) : 0;
-        int64_t run = len > 0 ? tiles_of(len) + PAIR_COST : 0;
+        int run = len > 0 ? tiles_of(len) + PAIR_COST : 0;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const int64_t y = __shfl_up_sync(0xffffffffu, run, o);
+            const int y = __shfl_up_sync(0xffffffffu, run, o);
             if (lane >= o) run += y;
         }
         const uint32_t past = __ballot_sync(0xffffffffu, before + run > x);
@@ -133,9 +134,9 @@ __device__ __forceinline__ void find_tile(const Params& p, int pairs, int64_t fi
             c.s = s0 + l;
             c.len = __shfl_sync(0xffffffffu, len, l);
             c.nt = tiles_of(c.len);
-            const int64_t seq0 = (before + __shfl_sync(0xffffffffu, run, l) - (c.nt + PAIR_COST)) * pairs;
-            c.pair = (int)quotient(first - seq0, c.nt + PAIR_COST);
-            c.begin = seq0 + (int64_t)c.pair * (c.nt + PAIR_COST);
+            const int seq0 = (before + __shfl_sync(0xffffffffu, run, l) - (c.nt + PAIR_COST)) * pairs;
+            c.pair = (first - seq0) / (c.nt + PAIR_COST);
+            c.begin = seq0 + c.pair * (c.nt + PAIR_COST);
             cut(c, first, end);
             return;
         }
@@ -143,13 +144,13 @@ __device__ __forceinline__ void find_tile(const Params& p, int pairs, int64_t fi
     }
 }
 // whole: the pair number c.begin or the next of my pairs that has keys.
-__device__ __forceinline__ void find_pair(const Params& p, int pairs, int64_t step, Cursor& c)
+__device__ __forceinline__ void find_pair(const Params& p, int pairs, int step, Cursor& c)
 {
     c.t = 0;
-    const int64_t n = (int64_t)p.n_seq * pairs;
+    const int n = p.n_seq * pairs;
     for (; c.begin < n; c.begin += step) {
-        c.s = (int)quotient(c.begin, pairs);
-        c.pair = (int)(c.begin - (int64_t)c.s * pairs);
+        c.s = c.begin / pairs;
+        c.pair = c.begin - c.s * pairs;
         c.len = len_of(p, c.s);
         c.n = c.nt = tiles_of(c.len);
         if (c.nt > 0) return;
@@ -157,7 +158,7 @@ __device__ __forceinline__ void find_pair(const Params& p, int pairs, int64_t st
     c.ok = false;
 }
 // From the end of my part of a pair to the next pair; `end`: of my share.
-__device__ __forceinline__ void next_pair(const Params& p, int pairs, int64_t step, int64_t end, Cursor& c)
+__device__ __forceinline__ void next_pair(const Params& p, int pairs, int step, int end, Cursor& c)
 {
     if (p.whole) { c.begin += step; find_pair(p, pairs, step, c); return; }
     c.begin += c.nt + PAIR_COST;
@@ -221,7 +222,7 @@ paged_kernel(const Params p)
     const int warps = R ? R : p.warps;
     const int warp_in_block = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31, g8 = lane >> 2, t4 = lane & 3;
     const int group = warp_in_block / warps, warp = warp_in_block - group * warps;
-    const int64_t n_groups = (int64_t)gridDim.x * (WARPS / warps), me = (int64_t)group * gridDim.x + blockIdx.x;
+    const int n_groups = gridDim.x * (WARPS / warps), me = group * gridDim.x + blockIdx.x;
     uint8_t* ring = smem + group * STAGES * stage;
     uint32_t* scratch = reinterpret_cast<uint32_t*>(smem + (WARPS / warps) * STAGES * stage + warp_in_block * scratch_bytes(BK, UN));
     const int pairs = p.H * p.chunks, slabs_per_page = p.P / SLAB;
@@ -234,21 +235,22 @@ paged_kernel(const Params p)
     pdl_wait();
 
     // rows of sequences without keys
-    for (int64_t s = me; s < p.n_seq; s += n_groups)
-        if (len_of(p, (int)s) == 0)
-            for (int i = 32 * warp + lane; i < p.H * p.G * p.d; i += 32 * warps) static_cast<uint16_t*>(p.out)[s * p.ldo + i] = 0;
+    for (int s = me; s < p.n_seq; s += n_groups)
+        if (len_of(p, s) == 0)
+            for (int i = 32 * warp + lane; i < p.H * p.G * p.d; i += 32 * warps) static_cast<uint16_t*>(p.out)[(int64_t)s * p.ldo + i] = 0;
 
     Cursor in{};                                           // what is loaded next
-    int64_t share = 0, end = 0;
+    int share = 0, end = 0;
     if (p.whole) {
         in.ok = true;
         in.begin = me;
         find_pair(p, pairs, n_groups, in);
     } else {
-        const int64_t total = list_per_pair(p) * pairs;
-        share = max(quotient(total + n_groups - 1, n_groups), (int64_t)p.min_share);
-        end = min((me + 1) * share, total);
-        if (me * share < total) find_tile(p, pairs, me * share, end, in);
+        const int total = find_shares(p, pairs, n_groups, share);
+        if (me <= (total - 1) / share) {
+            end = min(me * share + share, total);
+            find_tile(p, pairs, me * share, end, in);
+        }
     }
     if (!in.ok) return;
     Cursor c = in;                                         // what is worked on
@@ -635,7 +637,7 @@ paged_kernel(const Params p)
         const int h = c.pair / p.chunks, head0 = h * p.G + (c.pair - h * p.chunks) * (WARP_Q * warps) + WARP_Q * warp;
         const float2* val = p.val_v + (int64_t)h * nu * 32;
         const int pitch = part_pitch(nu);
-        auto part_of = [&](int64_t of, bool begins, int q) { return p.parts + (((of * 2 + begins) * warps + warp) * WARP_Q + q) * pitch; };
+        auto part_of = [&](int of, bool begins, int q) { return p.parts + (int64_t)(((of * 2 + begins) * warps + warp) * WARP_Q + q) * pitch; };
         flush(1.0f);
         float l = Fl + __shfl_xor_sync(0xffffffffu, Fl, 1);
         // a query that is not finite has no sum; nor has a pair none of whose pages exist, which gives zeros
@@ -674,8 +676,7 @@ paged_kernel(const Params p)
         }
         if (complete) return;
         // The pair's first tile is in the share of group g_first; the last of its parts to arrive joins them all, in the order of the shares.
-        const int64_t g_first = quotient(c.begin + PAIR_COST, share);
-        const int n_parts = (int)(quotient(c.begin + PAIR_COST + c.nt - 1, share) - g_first) + 1;
+        const int g_first = (c.begin + PAIR_COST) / share, n_parts = (c.begin + PAIR_COST + c.nt - 1) / share - g_first + 1;
         __threadfence();
         __syncwarp();
         int last = 0;
