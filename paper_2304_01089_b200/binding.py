@@ -257,25 +257,6 @@ _torch = None                    # set with the first KvCache
 _rows_types = {}                 # torch dtype -> RPTQ_ROWS_*
 
 
-def _rows(t, what: str, device: int, n_rows: int, n_cols: int):
-    """(pointer, elements between rows, RPTQ_ROWS_* type) of a 2-D CUDA tensor whose rows are contiguous."""
-    kind, shape, stride = _rows_types.get(t.dtype), t.shape, t.stride()
-    if kind is None:
-        raise ValueError(f"{what}: rows of {t.dtype} are not supported")
-    if t.get_device() != device or len(shape) != 2 or (stride[1] != 1 and shape[1] > 1):
-        raise ValueError(f"{what}: expected a 2-D tensor with contiguous rows on the cache's device")
-    if shape[0] < n_rows or shape[1] < n_cols:
-        raise ValueError(f"{what}: expected at least {n_rows} rows of {n_cols}, got {tuple(shape)}")
-    return t.data_ptr(), stride[0] if shape[0] > 1 else shape[1], kind
-
-
-def _ints(t, what: str, device: int, dtype, dim: int):
-    shape = t.shape
-    if t.dtype is not dtype or t.get_device() != device or len(shape) != dim or (shape[-1] > 1 and t.stride()[-1] != 1):
-        raise ValueError(f"{what}: expected a {dim}-D tensor of {dtype} on the cache's device")
-    return t.data_ptr()
-
-
 class KvCache:
     """rptq_kv_cache_create / _query / _destroy: what a paged key / value cache looks like. It owns no pages: a pool is a
     contiguous uint8 CUDA tensor of n_pages rows of k_page_bytes (v_page_bytes)."""
@@ -326,31 +307,46 @@ class KvCache:
 
 
 def _cache_rows(cache: KvCache, k, v, n: int):
-    codes = k.dtype is _torch.uint8
-    pk, ldk, kind = _rows(k, "k", cache.device, n, cache.k_row_bytes if codes else cache.C)
-    pv, ldv, kind_v = _rows(v, "v", cache.device, n, cache.v_row_bytes if codes else cache.C)
-    if kind != kind_v:
-        raise ValueError("k and v have different types")
-    return pk, ldk, pv, ldv, kind
+    """Pointers, distances and type of the rows of K and V in a call with n tokens."""
+    kind, ks, vs, kt, vt, device = _rows_types.get(k.dtype), k.shape, v.shape, k.stride(), v.stride(), cache.device
+    ck, cv = (cache.k_row_bytes, cache.v_row_bytes) if kind == ROWS_CODES else (cache.C, cache.C)
+    if kind is None or v.dtype is not k.dtype:
+        raise ValueError(f"k and v have one type, fp32, fp16, bf16 or uint8 code rows: got {k.dtype} and {v.dtype}")
+    if (len(ks) != 2 or len(vs) != 2 or ks[0] < n or vs[0] < n or ks[1] < ck or vs[1] < cv or (kt[1] != 1 and ks[1] > 1) or (vt[1] != 1 and vs[1] > 1)
+            or k.get_device() != device or v.get_device() != device):
+        raise ValueError(f"k and v: expected at least {n} contiguous rows of {ck} and {cv} on the cache's device, got {tuple(ks)} and {tuple(vs)}")
+    return k.data_ptr(), kt[0] if ks[0] > 1 else ks[1], v.data_ptr(), vt[0] if vs[0] > 1 else vs[1], kind
+
+
+def _slots(cache: KvCache, slots):
+    """Pointer and number of a call's slots."""
+    shape = slots.shape
+    if slots.dtype is not _torch.int64 or len(shape) != 1 or slots.get_device() != cache.device or not slots.is_contiguous():
+        raise ValueError("slots: expected a contiguous 1-D tensor of int64 on the cache's device")
+    return slots.data_ptr(), shape[0]
 
 
 def kv_cache_write(cache: KvCache, k, v, slots, k_pages, v_pages, stream=None) -> None:
     """rptq_kv_cache_write: k, v [n][>= C] of fp16, bf16 or fp32 (original channel order; rows may lie apart, as in a slice of a fused
     projection's output), or uint8 code rows [n][>= row_bytes] of the layouts; slots int64 [n] (negative: skipped);
     k_pages, v_pages uint8 [n_pages][page bytes]. CUDA tensors."""
-    at, n = _ints(slots, "slots", cache.device, _torch.int64, 1), slots.shape[0]
+    at, n = _slots(cache, slots)
     kp, vp, n_pages = cache.pools(k_pages, v_pages)
     pk, ldk, pv, ldv, kind = _cache_rows(cache, k, v, n)
-    _check(_lib.rptq_kv_cache_write(cache.handle, pk, ldk, pv, ldv, kind, at, n, kp, vp, n_pages, _stream_ptr(stream)), "rptq_kv_cache_write")
+    status = _lib.rptq_kv_cache_write(cache.handle, pk, ldk, pv, ldv, kind, at, n, kp, vp, n_pages, _stream_ptr(stream))
+    if status != OK:
+        raise RptqError(status, "rptq_kv_cache_write")
 
 
 def kv_cache_read(cache: KvCache, k_pages, v_pages, slots, k_out, v_out, stream=None) -> None:
     """rptq_kv_cache_read: row i of k_out, v_out (fp16, bf16, fp32 [n][>= C], or uint8 code rows [n][>= row_bytes]) receives slot
     slots[i]; rows of negative slots stay as they are."""
-    at, n = _ints(slots, "slots", cache.device, _torch.int64, 1), slots.shape[0]
+    at, n = _slots(cache, slots)
     kp, vp, n_pages = cache.pools(k_pages, v_pages)
     pk, ldk, pv, ldv, kind = _cache_rows(cache, k_out, v_out, n)
-    _check(_lib.rptq_kv_cache_read(cache.handle, kp, vp, n_pages, at, n, pk, ldk, pv, ldv, kind, _stream_ptr(stream)), "rptq_kv_cache_read")
+    status = _lib.rptq_kv_cache_read(cache.handle, kp, vp, n_pages, at, n, pk, ldk, pv, ldv, kind, _stream_ptr(stream))
+    if status != OK:
+        raise RptqError(status, "rptq_kv_cache_read")
 
 
 def attention_paged_workspace_bytes(cache: KvCache, n_q_heads: Optional[int] = None) -> int:
@@ -369,24 +365,30 @@ def attention_paged(cache: KvCache, q, k_pages, v_pages, page_table, seq_lens, o
     """rptq_attention_paged: q, out fp16 or bf16 [n_seq][>= n_q_heads * d], page_table int32 [n_seq][pages], seq_lens int32 [n_seq]; CUDA
     tensors. n_q_heads: a multiple of the cache's heads (default: as many). workspace: a contiguous tensor of at least
     attention_paged_workspace_bytes(cache, n_q_heads) bytes, allocated by the call if None."""
-    n_q_heads, device = cache.n_heads if n_q_heads is None else int(n_q_heads), cache.device
-    lens, n_seq = _ints(seq_lens, "seq_lens", device, _torch.int32, 1), seq_lens.shape[0]
+    if n_q_heads is None:
+        n_q_heads = cache.n_heads
+    device, dtype, cols = cache.device, q.dtype, n_q_heads * cache.head_dim
+    kind, qs, os, qt, ot, ls, ts, tt = _rows_types.get(dtype), q.shape, out.shape, q.stride(), out.stride(), seq_lens.shape, page_table.shape, page_table.stride()
+    n_seq = ls[0] if len(ls) == 1 else -1
+    if kind is None or out.dtype is not dtype:
+        raise ValueError(f"q and out have one type, fp16 or bf16: got {dtype} and {out.dtype}")
+    if (len(qs) != 2 or len(os) != 2 or qs[0] < n_seq or os[0] < n_seq or qs[1] < cols or os[1] < cols or (qt[1] != 1 and qs[1] > 1) or (ot[1] != 1 and os[1] > 1)
+            or q.get_device() != device or out.get_device() != device):
+        raise ValueError(f"q and out: expected at least {n_seq} contiguous rows of {cols} on the cache's device, got {tuple(qs)} and {tuple(os)}")
+    if (n_seq < 0 or len(ts) != 2 or ts[0] < n_seq or (tt[1] != 1 and ts[1] > 1) or seq_lens.dtype is not _torch.int32 or page_table.dtype is not _torch.int32
+            or seq_lens.get_device() != device or page_table.get_device() != device or not seq_lens.is_contiguous()):
+        raise ValueError(f"seq_lens [n_seq] and page_table [n_seq][pages] are int32 on the cache's device, got {seq_lens.dtype} {tuple(ls)} and {page_table.dtype} {tuple(ts)}")
     kp, vp, n_pages = cache.pools(k_pages, v_pages)
-    cols = n_q_heads * cache.head_dim
-    pq, ldq, kind = _rows(q, "q", device, n_seq, cols)
-    po, ldo, kind_o = _rows(out, "out", device, n_seq, cols)
-    if kind != kind_o:
-        raise ValueError("q and out have different types")
-    table, (n_rows, width) = _ints(page_table, "page_table", device, _torch.int32, 2), page_table.shape
-    if n_rows < n_seq:
-        raise ValueError("page_table has fewer rows than there are sequences")
     need = attention_paged_workspace_bytes(cache, n_q_heads)
     if workspace is None:
         workspace = _torch.empty(need, dtype=_torch.uint8, device=q.device)
-    if workspace.nbytes < need or not workspace.is_contiguous() or workspace.get_device() != device:
+    elif workspace.nbytes < need or not workspace.is_contiguous() or workspace.get_device() != device:
         raise ValueError(f"workspace: {need} contiguous bytes on the cache's device are needed")
-    _check(_lib.rptq_attention_paged(cache.handle, pq, ldq, kind, n_q_heads, n_seq, kp, vp, n_pages, table, page_table.stride(0) if n_rows > 1 else width,
-                                     width, lens, qk_scale, po, ldo, workspace.data_ptr(), _stream_ptr(stream)), "rptq_attention_paged")
+    status = _lib.rptq_attention_paged(cache.handle, q.data_ptr(), qt[0] if qs[0] > 1 else qs[1], kind, n_q_heads, n_seq, kp, vp, n_pages, page_table.data_ptr(),
+                                       tt[0] if ts[0] > 1 else ts[1], ts[1], seq_lens.data_ptr(), qk_scale, out.data_ptr(), ot[0] if os[0] > 1 else os[1],
+                                       workspace.data_ptr(), _stream_ptr(stream))
+    if status != OK:
+        raise RptqError(status, "rptq_attention_paged")
 
 
 def weight_pack(layout_in: Layout, W: np.ndarray, out_perm=None, n_pad: Optional[int] = None):

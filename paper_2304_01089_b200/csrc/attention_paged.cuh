@@ -344,7 +344,7 @@ paged_kernel(const Params p)
 #pragma unroll
         for (int i = 0; i < UN; ++i) {
             const int ch = 32 * i + lane;
-            k_scale[i] = i < nu && n > 0 ? val[ch].x : 0.f;
+            k_scale[i] = i < nu && n > 0 ? __ldg(&val[ch].x) : 0.f;
             q_bits[i] = ch < p.d && n > 0 ? query_bits(p, of.s, h * p.G + q0, ch) : 0u;
             if (ch < p.d && n > 1) q_bits[i] |= (uint32_t)query_bits(p, of.s, h * p.G + q0 + 1, ch) << 16;
         }
@@ -665,7 +665,7 @@ paged_kernel(const Params p)
                 if (!mine || ch >= 32 * nu) continue;
                 float y[N];
 #pragma unroll
-                for (int i = 0; i < N; ++i) y[i] = complete ? result(o[N * x + i], l, inv, val[ch + i]) : o[N * x + i];
+                for (int i = 0; i < N; ++i) y[i] = complete ? result(o[N * x + i], l, inv, __ldg(val + ch + i)) : o[N * x + i];
                 if (complete) {
                     store_out<N>(p, c.s, head0 + q, ch, y);
                 } else {
@@ -699,8 +699,13 @@ paged_kernel(const Params p)
         constexpr int AHEAD = UN <= 4 ? 8 : 4, V = UN <= 4 ? 1 : 2;                          // four channels a lane, twice
         const int all = n_parts * n_heads;
         float4 o[V];
+        float2 sz[V][4];
         float top = NO_REF;
         int head = 0, i = 0;                                                   // head and part of the next sum
+#pragma unroll
+        for (int x = 0; x < V; ++x)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) sz[x][k] = __ldg(val + min(4 * lane + 128 * x, 32 * nu - 4) + k);
         l = 0.f;
 #pragma unroll
         for (int x = 0; x < V; ++x) o[x] = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -733,8 +738,8 @@ paged_kernel(const Params p)
                 for (int x = 0; x < V; ++x) {
                     const int ch = 4 * lane + 128 * x;
                     if (ch >= 32 * nu) continue;
-                    const float y[4] = {result(o[x].x, l, to_one, val[ch]), result(o[x].y, l, to_one, val[ch + 1]), result(o[x].z, l, to_one, val[ch + 2]),
-                                        result(o[x].w, l, to_one, val[ch + 3])};
+                    const float y[4] = {result(o[x].x, l, to_one, sz[x][0]), result(o[x].y, l, to_one, sz[x][1]), result(o[x].z, l, to_one, sz[x][2]),
+                                        result(o[x].w, l, to_one, sz[x][3])};
                     store_out<4>(p, c.s, head0 + head, ch, y);
                     o[x] = make_float4(0.f, 0.f, 0.f, 0.f);
                 }
