@@ -1,6 +1,7 @@
 // rptq_attention_paged: argument checks, the choice of the kernel's instance, and the launches. The kernel: attention_paged.cuh.
 #include <chrono>
 #include <climits>
+#include <cmath>
 
 #include "attention_paged.cuh"
 #include "attention_paged_launch.h"
@@ -56,7 +57,7 @@ int rptq_attention_paged(const rptq_kv_cache_t* cache, const void* q, int64_t ld
 {
     using namespace rptq;
     using namespace rptq::attn_paged;
-    if (!cache || n_seq < 0 || n_pages < 0 || table_width < 0 || !(qk_scale >= 0.f)) return RPTQ_ERR_INVALID_ARG;
+    if (!cache || n_seq < 0 || n_pages < 0 || table_width < 0 || !(qk_scale >= 0.f) || !std::isfinite(qk_scale)) return RPTQ_ERR_INVALID_ARG;
     if (n_q_heads < 1 || n_q_heads % cache->H || ld_table < table_width) return RPTQ_ERR_INVALID_ARG;
     if (q_type != RPTQ_ROWS_F16 && q_type != RPTQ_ROWS_BF16) return RPTQ_ERR_INVALID_ARG;
     const int64_t Cq = (int64_t)n_q_heads * cache->d;

@@ -46,6 +46,7 @@ constexpr int TILE = 2 * SLAB;                 // keys
 constexpr int WARPS = 4, THREADS = 32 * WARPS;  // of a block: 4, 2 or 1 groups
 constexpr int PAIR_COST = 4;                   // tiles that beginning and ending a pair counts as
 constexpr int WARP_Q = 2;                      // query heads of a warp
+constexpr int MAX_TRIES = 1 << 14;             // (every failed one is another group's success, of which there are a few per part)
 constexpr float HEAD = 4.0f;                   // how far above the largest score a moved reference lies, in powers of two
 constexpr float NO_REF = -1.0e30f;
 constexpr int FLUSH_TILES = 1000;              // 32 keys x 255 x 255 a tile stay below 2^31 in 32-bit sums for 1032 tiles
@@ -685,12 +686,13 @@ paged_kernel(const Params p)
             // in its place.
             unsigned long long* at = p.arrived + g_first * warps + warp;
             unsigned long long before = atomicAdd(at, 1ull);
-            while ((before & ~0xFFFFull) != p.mark) {
+            for (int tries = 0; (before & ~0xFFFFull) != p.mark && tries < MAX_TRIES; ++tries) {
                 const unsigned long long seen = *reinterpret_cast<volatile unsigned long long*>(at);
                 if ((seen & ~0xFFFFull) == p.mark) before = atomicAdd(at, 1ull);
                 else if (atomicCAS(at, seen, p.mark + 1) == seen) before = p.mark;
             }
-            last = (int)(before & 0xFFFF) == n_parts - 1;
+            last = before == p.mark + (unsigned)(n_parts - 1);
+            if ((before & ~0xFFFFull) != p.mark && p.status) *p.status = RPTQ_ERR_DEVICE_TIMEOUT;
             if (last) *reinterpret_cast<volatile unsigned long long*>(at) = p.mark;
         }
         if (!__shfl_sync(0xffffffffu, last, 0)) return;

@@ -227,6 +227,11 @@ def test_attention_long_sequences_are_split(G, bits):
     Batch(501 + G, 2, 128, bits, 16, [3001, 40, 2500], G=G, dtype="bf16").check()
 
 
+@pytest.mark.parametrize("bits,G", [((4, 4), 1), ((8, 8), 8)])
+def test_attention_one_head_over_a_very_long_sequence(bits, G):
+    Batch(506, 1, 128, bits, 256, [70000], G=G).check()
+
+
 def test_attention_many_sequences():
     rng = np.random.default_rng(3)
     Batch(510, 3, 64, (4, 4), 16, rng.integers(0, 200, size=300)).check()
@@ -419,6 +424,30 @@ def test_on_other_streams_and_in_a_graph():
         torch.cuda.synchronize()
         want, bound = b.want()
         assert (np.abs(out.double().cpu().numpy() - want) <= bound).all()
+    assert binding.get_device_status() == 0
+
+
+def test_two_graphs_that_share_a_workspace():
+    """Captured over the same workspace and replayed by turns, with other work over it in between: what a call finds there does not matter."""
+    import torch
+    from paper_2304_01089_b200 import binding
+    b = [Batch(625, 2, 128, (4, 4), 16, [5000, 70]), Batch(626, 1, 64, (8, 8), 32, [9000], G=4), Batch(627, 3, 96, (3, 3), 16, [700, 0, 33], G=2)]
+    want = [x.check() for x in b]
+    ws = torch.randint(0, 256, (max(binding.attention_paged_workspace_bytes(x.site.cache, x.site.H * x.G) for x in b),), dtype=torch.uint8, device="cuda")
+    outs, graphs = [torch.empty_like(x.q) for x in b], []
+    for x, o in zip(b, outs):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            binding.attention_paged(x.site.cache, x.q, *x.pools, x.table_dev, x.lens_dev, o, x.qk_scale, n_q_heads=x.site.H * x.G, workspace=ws)
+        graphs.append(g)
+    for turn in range(6):
+        if turn in (2, 4):
+            ws.random_(0, 256)
+        for i in ((0, 1, 2), (2, 1, 0), (1, 1, 0, 2))[turn % 3]:
+            outs[i].fill_(float("nan"))
+            graphs[i].replay()
+            torch.cuda.synchronize()
+            assert torch.equal(outs[i], want[i])
     assert binding.get_device_status() == 0
 
 

@@ -88,9 +88,10 @@ def test_attention_refuses(binding):
 
     for kw in [dict(cache=None), dict(q=None), dict(out=None), dict(kp=None), dict(vp=None), dict(table=None), dict(lens=None), dict(ws=None), dict(seqs=-1), dict(pages=-1),
                dict(width=-1), dict(ldt=4), dict(heads=0), dict(heads=3), dict(ldq=255), dict(ldo=255), dict(kind=binding.ROWS_F32), dict(kind=binding.ROWS_CODES),
-               dict(q=ODD), dict(out=ODD), dict(kp=A + 4), dict(vp=A + 4), dict(table=A + 2), dict(lens=A + 2), dict(ws=A + 8), dict(scale=-1.0), dict(scale=float("nan"))]:
+               dict(q=ODD), dict(out=ODD), dict(kp=A + 4), dict(vp=A + 4), dict(table=A + 2), dict(lens=A + 2), dict(ws=A + 8), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf"))]:
         assert call(**kw) == inv, kw
     assert call(seqs=65536) == uns and call(width=1 << 28, ldt=1 << 28) == uns
+    assert call(seqs=60000, width=1 << 16, ldt=1 << 16) == uns             # more tiles than the list has places
     assert call(seqs=0, q=None) == binding.OK
     if not torch.cuda.is_available():
         assert call() == binding.ERR_CUDA
