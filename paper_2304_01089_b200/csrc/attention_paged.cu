@@ -48,7 +48,7 @@ int64_t rptq_attention_paged_workspace_bytes(const rptq_kv_cache_t* cache, int n
     const int n_sm = cache->device < 0 ? 0 : sm_count(cache->device);
     if (n_sm == 0) return RPTQ_ERR_CUDA;
     const Plan x = plan_of(cache, n_q_heads / cache->H);
-    return (int64_t)n_sm * x.blocks_per_sm * WARPS * (8 + 2 * WARP_Q * 4 * part_pitch(cache->nu));
+    return (int64_t)n_sm * x.blocks_per_sm * WARPS * (3 * 8 + 2 * WARP_Q * 4 * part_pitch(cache->nu));
 }
 
 int rptq_attention_paged(const rptq_kv_cache_t* cache, const void* q, int64_t ldq, int q_type, int n_q_heads, int n_seq,
@@ -95,7 +95,7 @@ int rptq_attention_paged(const rptq_kv_cache_t* cache, const void* q, int64_t ld
     p.status = device_status_word();
     p.warps = x.warps;
     const int64_t most = (int64_t)n_sm * x.blocks_per_sm;
-    p.parts = reinterpret_cast<float*>(p.arrived + most * WARPS);
+    p.parts = reinterpret_cast<float*>(p.arrived + 3 * most * WARPS);
 
     // a grid that fills the GPU is the most
     p.whole = max_tiles <= WHOLE_TILES;

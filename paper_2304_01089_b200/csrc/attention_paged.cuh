@@ -46,6 +46,7 @@ constexpr int TILE = 2 * SLAB;                 // keys
 constexpr int WARPS = 4, THREADS = 32 * WARPS;  // of a block: 4, 2 or 1 groups
 constexpr int PAIR_COST = 4;                   // tiles that beginning and ending a pair counts as
 constexpr int WARP_Q = 2;                      // query heads of a warp
+constexpr int MANY_PARTS = 32;                 // more parts of a pair than these are joined in two levels
 constexpr int MAX_TRIES = 1 << 14;             // (every failed one is another group's success, of which there are a few per part)
 constexpr float HEAD = 4.0f;                   // how far above the largest score a moved reference lies, in powers of two
 constexpr float NO_REF = -1.0e30f;
@@ -74,8 +75,10 @@ struct Params {
     int whole;                                 // a group takes whole pairs, every n-th; nothing is split
     int min_share;                             // least share of a group
     float scale_log2e;
-    unsigned long long* arrived;               // [groups][warps] parts that are there of the pair that began in the group's share and goes on, under MARK
-    unsigned long long mark;                   // the process's mark in them, its lowest 16 bits zero
+    // [groups][3][warps] parts that are there, under the process's mark: of the run of parts that begins with the group's part of the pair which
+    // comes into its share from before; of the run that begins with its part of the pair which begins there; and of the latter pair's runs
+    unsigned long long* arrived;
+    unsigned long long mark;                   // its lowest 16 bits are zero
     float* parts;                              // [groups][2][warps][WARP_Q][4 + 32 nu]: reference, sum, -, -, outputs of a pair's part
     int* status;
 };
@@ -90,20 +93,16 @@ struct Cursor {
     bool ok;
 };
 
-// All lanes: a group's share of the list, and the list's length. Equal shares, but not less than min_share, nor so little that the
-// longest pair falls into many more parts than one warp joins in the time of its tiles: of n parts of nt tiles that takes about nt / n x 0.5 us and
-// n / 8 x 1.2 us, the least when a part has sqrt(0.3 nt). (The host sees to it that the list and its places stay below 2^31.)
+// All lanes: a group's share of the list, and the list's length. (The host sees to it that the list and its places stay below 2^31.)
 __device__ __forceinline__ int find_shares(const Params& p, int pairs, int n_groups, int& share)
 {
-    int n = 0, longest = 0;
+    int n = 0;
     for (int s = threadIdx.x & 31; s < p.n_seq; s += 32) {
         const int nt = tiles_of(len_of(p, s));
         n += nt > 0 ? nt + PAIR_COST : 0;
-        longest = max(longest, nt);
     }
     const int total = __reduce_add_sync(0xffffffffu, n) * pairs;
-    longest = __reduce_max_sync(0xffffffffu, longest);
-    share = max(max((total + n_groups - 1) / n_groups, p.min_share), PAIR_COST + (int)sqrtf(0.3f * (float)longest));
+    share = max((total + n_groups - 1) / n_groups, p.min_share);
     return total;
 }
 // My tiles of the pair c.s, c.pair, which begins at c.begin: those at places first .. end - 1 of the list.
@@ -676,77 +675,92 @@ paged_kernel(const Params p)
             }
         }
         if (complete) return;
-        // The pair's first tile is in the share of group g_first; the last of its parts to arrive joins them all, in the order of the shares.
+        // The pair's first tile is in the share of group g_first. The last of its parts to arrive joins them, in the order of the shares. Many
+        // parts are joined in runs first, by the last of each run, and the run's sum takes the place of its first part.
         const int g_first = (c.begin + PAIR_COST) / share, n_parts = (c.begin + PAIR_COST + c.nt - 1) / share - g_first + 1;
-        __threadfence();
-        __syncwarp();
-        int last = 0;
-        if (lane == 0) {
-            // A count is 0 again after every call. What is no count of this process lacks its mark: one of those that come first puts a count
-            // in its place.
-            unsigned long long* at = p.arrived + g_first * warps + warp;
-            unsigned long long before = atomicAdd(at, 1ull);
-            for (int tries = 0; (before & ~0xFFFFull) != p.mark && tries < MAX_TRIES; ++tries) {
-                const unsigned long long seen = *reinterpret_cast<volatile unsigned long long*>(at);
-                if ((seen & ~0xFFFFull) == p.mark) before = atomicAdd(at, 1ull);
-                else if (atomicCAS(at, seen, p.mark + 1) == seen) before = p.mark;
-            }
-            last = before == p.mark + (unsigned)(n_parts - 1);
-            if ((before & ~0xFFFFull) != p.mark && p.status) *p.status = RPTQ_ERR_DEVICE_TIMEOUT;
-            if (last) *reinterpret_cast<volatile unsigned long long*>(at) = p.mark;
-        }
-        if (!__shfl_sync(0xffffffffu, last, 0)) return;
-        __threadfence();
-        // all parts of both heads in a row, some of them under way; a running reference as for the tiles
-        constexpr int AHEAD = UN <= 4 ? 8 : 4, V = UN <= 4 ? 1 : 2;                          // four channels a lane, twice
-        const int all = n_parts * n_heads;
-        float4 o[V];
-        float2 sz[V][4];
-        float top = NO_REF;
-        int head = 0, i = 0;                                                   // head and part of the next sum
-#pragma unroll
-        for (int x = 0; x < V; ++x)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) sz[x][k] = __ldg(val + min(4 * lane + 128 * x, 32 * nu - 4) + k);
-        l = 0.f;
-#pragma unroll
-        for (int x = 0; x < V; ++x) o[x] = make_float4(0.f, 0.f, 0.f, 0.f);
+        const int run = n_parts <= MANY_PARTS ? 1 : ((int)sqrtf((float)n_parts) + 8) & ~7;
 #pragma unroll 1
-        for (int n0 = 0; n0 < all; n0 += AHEAD) {
-            float4 v[AHEAD][V];
-            float2 sums[AHEAD];
-#pragma unroll
-            for (int k = 0; k < AHEAD; ++k) {
-                const int n = min(n0 + k, all - 1), qn = n >= n_parts, b = n - (qn ? n_parts : 0);
-                const float* from = part_of(g_first + b, b == 0, qn);
-                sums[k] = __ldcg(reinterpret_cast<const float2*>(from));
-#pragma unroll
-                for (int x = 0; x < V; ++x) v[k][x] = __ldcg(reinterpret_cast<const float4*>(from + 4 + min(4 * lane + 128 * x, 32 * nu - 4)));
+        for (int level = run == 1 ? 1 : 0; level < 2; ++level) {
+            // what I may have to join: `count` parts, `step` apart, or the runs' sums
+            const int from = level == 0 ? (me - g_first) / run * run : 0;
+            const int step = level == 0 ? 1 : run, count = level == 0 ? min(run, n_parts - from) : (n_parts + run - 1) / run;
+            __threadfence();
+            __syncwarp();
+            int last = 0;
+            if (lane == 0) {
+                // A count is 0 again after every call. What is no count of this process lacks its mark: one of those that come first puts a
+                // count in its place.
+                unsigned long long* at = p.arrived + ((g_first + from) * 3 + (level == 1 ? 2 : from == 0)) * warps + warp;
+                unsigned long long before = atomicAdd(at, 1ull);
+                for (int tries = 0; (before & ~0xFFFFull) != p.mark && tries < MAX_TRIES; ++tries) {
+                    const unsigned long long seen = *reinterpret_cast<volatile unsigned long long*>(at);
+                    if ((seen & ~0xFFFFull) == p.mark) before = atomicAdd(at, 1ull);
+                    else if (atomicCAS(at, seen, p.mark + 1) == seen) before = p.mark;
+                }
+                last = before == p.mark + (unsigned)(count - 1);
+                if ((before & ~0xFFFFull) != p.mark && p.status) *p.status = RPTQ_ERR_DEVICE_TIMEOUT;
+                if (last) *reinterpret_cast<volatile unsigned long long*>(at) = p.mark;
             }
+            if (!__shfl_sync(0xffffffffu, last, 0)) return;
+            __threadfence();
+            // the parts of both heads in a row, AHEAD of them under way; a running reference as for the tiles
+            constexpr int AHEAD = UN <= 4 ? 8 : 4, V = UN <= 4 ? 1 : 2;        // four channels a lane, twice
+            const int all = count * n_heads;
+            float4 o[V];
+            float2 sz[V][4];
+            float top = NO_REF;
+            int head = 0, i = 0;                                               // head and part of the next sum
 #pragma unroll
-            for (int k = 0; k < AHEAD; ++k) {
-                if (n0 + k >= all) break;
-                const float to = fmaxf(top, sums[k].x), f = ex2(fmaxf(top - to, -1000.0f)), g = ex2(fmaxf(sums[k].x - to, -1000.0f));
-                top = to;
-                l = __fmaf_rn(g, sums[k].y, f * l);
+            for (int x = 0; x < V; ++x)
 #pragma unroll
-                for (int x = 0; x < V; ++x) {
-                    o[x].x = __fmaf_rn(g, v[k][x].x, f * o[x].x); o[x].y = __fmaf_rn(g, v[k][x].y, f * o[x].y);
-                    o[x].z = __fmaf_rn(g, v[k][x].z, f * o[x].z); o[x].w = __fmaf_rn(g, v[k][x].w, f * o[x].w);
+                for (int k = 0; k < 4; ++k) sz[x][k] = __ldg(val + min(4 * lane + 128 * x, 32 * nu - 4) + k);
+            l = 0.f;
+#pragma unroll
+            for (int x = 0; x < V; ++x) o[x] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+            for (int n0 = 0; n0 < all; n0 += AHEAD) {
+                float4 v[AHEAD][V];
+                float2 sums[AHEAD];
+#pragma unroll
+                for (int k = 0; k < AHEAD; ++k) {
+                    const int n = min(n0 + k, all - 1), second = n >= count, b = from + (n - (second ? count : 0)) * step;
+                    const float* at = part_of(g_first + b, b == 0, second);
+                    sums[k] = __ldcg(reinterpret_cast<const float2*>(at));
+#pragma unroll
+                    for (int x = 0; x < V; ++x) v[k][x] = __ldcg(reinterpret_cast<const float4*>(at + 4 + min(4 * lane + 128 * x, 32 * nu - 4)));
                 }
-                if (++i < n_parts) continue;
-                const float to_one = 1.0f / l;
 #pragma unroll
-                for (int x = 0; x < V; ++x) {
-                    const int ch = 4 * lane + 128 * x;
-                    if (ch >= 32 * nu) continue;
-                    const float y[4] = {result(o[x].x, l, to_one, sz[x][0]), result(o[x].y, l, to_one, sz[x][1]), result(o[x].z, l, to_one, sz[x][2]),
-                                        result(o[x].w, l, to_one, sz[x][3])};
-                    store_out<4>(p, c.s, head0 + head, ch, y);
-                    o[x] = make_float4(0.f, 0.f, 0.f, 0.f);
+                for (int k = 0; k < AHEAD; ++k) {
+                    if (n0 + k >= all) break;
+                    const float to = fmaxf(top, sums[k].x), f = ex2(fmaxf(top - to, -1000.0f)), g = ex2(fmaxf(sums[k].x - to, -1000.0f));
+                    top = to;
+                    l = __fmaf_rn(g, sums[k].y, f * l);
+#pragma unroll
+                    for (int x = 0; x < V; ++x) {
+                        o[x].x = __fmaf_rn(g, v[k][x].x, f * o[x].x); o[x].y = __fmaf_rn(g, v[k][x].y, f * o[x].y);
+                        o[x].z = __fmaf_rn(g, v[k][x].z, f * o[x].z); o[x].w = __fmaf_rn(g, v[k][x].w, f * o[x].w);
+                    }
+                    if (++i < count) continue;
+                    float* sum = part_of(g_first + from, from == 0, head);
+                    if (level == 0 && lane == 0) *reinterpret_cast<float2*>(sum) = make_float2(top, l);
+                    const float to_one = 1.0f / l;
+#pragma unroll
+                    for (int x = 0; x < V; ++x) {
+                        const int ch = 4 * lane + 128 * x;
+                        if (ch < 32 * nu) {
+                            if (level == 0) {
+                                *reinterpret_cast<float4*>(sum + 4 + ch) = o[x];
+                            } else {
+                                const float y[4] = {result(o[x].x, l, to_one, sz[x][0]), result(o[x].y, l, to_one, sz[x][1]), result(o[x].z, l, to_one, sz[x][2]),
+                                                    result(o[x].w, l, to_one, sz[x][3])};
+                                store_out<4>(p, c.s, head0 + head, ch, y);
+                            }
+                        }
+                        o[x] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    }
+                    top = NO_REF; l = 0.f; i = 0;
+                    ++head;
                 }
-                top = NO_REF; l = 0.f; i = 0;
-                ++head;
             }
         }
     };
