@@ -5,6 +5,8 @@
 // registers. Tokens whose slots follow one another inside a group of four keys (a prompt's, whatever key it starts at) are taken together: the
 // bytes of V that one token owns lie four apart, but four tokens' bytes of a word are 16 in a row (a 4 x 4 transposition in registers). One
 // token alone writes its bytes one by one.
+// The next group's loads are under way while a group is worked on. Rows of values are read and written past the caches (they are
+// used once; with the default policy the longest timed case took 77 us).
 // LATER
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -152,7 +154,7 @@ __device__ __forceinline__ Raw<T> load8(const T* from, int real)
     Raw<T> r;
     if constexpr (VECTOR) {
 #pragma unroll
-        for (int i = 0; i < Raw<T>::N; ++i) r.v[i] = real > 0 ? reinterpret_cast<const uint4*>(from)[i] : make_uint4(0, 0, 0, 0);
+        for (int i = 0; i < Raw<T>::N; ++i) r.v[i] = real > 0 ? __ldcs(reinterpret_cast<const uint4*>(from) + i) : make_uint4(0, 0, 0, 0);
     } else {
         T e[8];
 #pragma unroll
@@ -372,10 +374,10 @@ __device__ __forceinline__ void read_rows(const Params& p, const Side& s, int fi
             if (at.real == 0) continue;
             if constexpr (VECTOR) {
                 if constexpr (std::is_same<T, float>::value) {
-                    reinterpret_cast<float4*>(row)[0] = make_float4(y[0].x, y[0].y, y[1].x, y[1].y);
-                    reinterpret_cast<float4*>(row)[1] = make_float4(y[2].x, y[2].y, y[3].x, y[3].y);
+                    __stcs(reinterpret_cast<float4*>(row), make_float4(y[0].x, y[0].y, y[1].x, y[1].y));
+                    __stcs(reinterpret_cast<float4*>(row) + 1, make_float4(y[2].x, y[2].y, y[3].x, y[3].y));
                 } else {
-                    *reinterpret_cast<uint4*>(row) = make_uint4(join2(y[0], T()), join2(y[1], T()), join2(y[2], T()), join2(y[3], T()));
+                    __stcs(reinterpret_cast<uint4*>(row), make_uint4(join2(y[0], T()), join2(y[1], T()), join2(y[2], T()), join2(y[3], T())));
                 }
             } else {
 #pragma unroll
@@ -401,11 +403,11 @@ __device__ __forceinline__ void read_rows(const Params& p, const Side& s, int fi
 }
 
 // A warp takes a chunk of 256 channels of K or V (blockIdx.y) and a window of the tokens; the four warps of a block take neighbouring
-// chunks. Six blocks per SM (80 registers; rows of fp32 four, 128). (Parts as long as make all warps resident at once, K's and V's at the same
+// chunks. Six blocks per SM write (80 registers; rows of fp32 four, 128), eight read (64). (Parts as long as make all warps resident at once, K's and V's at the same
 // time, were 15 % slower: 90 us against 77 for the longest timed case.)
-template <class T> constexpr int rows_blocks_per_sm() { return sizeof(T) == 4 ? 4 : 6; }
+template <class T> constexpr int rows_blocks_per_sm(bool write) { return !write ? 8 : sizeof(T) == 4 ? 4 : 6; }
 template <class T, bool WRITE>
-__global__ void __launch_bounds__(THREADS, rows_blocks_per_sm<T>()) rows_kernel(const Params p)
+__global__ void __launch_bounds__(THREADS, rows_blocks_per_sm<T>(WRITE)) rows_kernel(const Params p)
 {
     pdl_trigger();
     if constexpr (WRITE) pdl_wait();                       // (inside, behind the loads of the parameters, it costs the write's instances registers)
