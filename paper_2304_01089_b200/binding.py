@@ -253,8 +253,18 @@ def attention_kv(LK: Layout, LV: Layout, n_heads: int, q, k_codes, v_codes, out,
                                   _dev_ptr(out), int(out.stride(0)), _stream_ptr(stream)), "rptq_attention_kv")
 
 
-_torch = None                    # set with the first KvCache
-_rows_types = {}                 # torch dtype -> RPTQ_ROWS_*
+_calls = None                    # the module that hands tensors to the paged cache's functions (csrc/calls.cpp); loaded with the first KvCache
+
+
+def _load_calls():
+    global _calls
+    if _calls is None:
+        import torch  # noqa: F401  (its libraries are what the module is linked with)
+        try:
+            from . import _calls as module
+        except ImportError as e:
+            raise ImportError("_calls.so is missing or does not fit the installed PyTorch: build it with `python -m paper_2304_01089_b200.build`") from e
+        _calls = module
 
 
 class KvCache:
@@ -262,22 +272,21 @@ class KvCache:
     contiguous uint8 CUDA tensor of n_pages rows of k_page_bytes (v_page_bytes)."""
 
     def __init__(self, layout_k: Layout, layout_v: Layout, n_heads: int, page_size: int):
-        global _torch
-        if _torch is None:
-            import torch
-            _rows_types.update({torch.float32: ROWS_F32, torch.float16: ROWS_F16, torch.uint8: ROWS_CODES, torch.bfloat16: ROWS_BF16})
-            _torch = torch
+        import torch
+        _load_calls()
+        self._call = None
         h = C.c_void_p()
         _check(_lib.rptq_kv_cache_create(C.byref(h), layout_k.handle, layout_v.handle, int(n_heads), int(page_size)), "rptq_kv_cache_create")
         self._h = h
         self.C, self.n_heads, self.page_size = layout_k.C, int(n_heads), int(page_size)
         self.head_dim = self.C // self.n_heads
-        self.device = _torch.cuda.current_device() if _torch.cuda.is_available() else -1
+        self.device = torch.cuda.current_device() if torch.cuda.is_available() else -1
         self.k_row_bytes, self.v_row_bytes = layout_k.row_bytes, layout_v.row_bytes
         kb, vb = C.c_int64(), C.c_int64()
         _check(_lib.rptq_kv_cache_query(self._h, C.byref(kb), C.byref(vb)), "rptq_kv_cache_query")
         self.k_page_bytes, self.v_page_bytes = int(kb.value), int(vb.value)
         self._workspace = {}                               # query heads -> bytes
+        self._call = _calls.describe(h.value, self.C, self.head_dim, self.k_row_bytes, self.v_row_bytes, self.k_page_bytes, self.v_page_bytes, self.device)
 
     @property
     def handle(self) -> C.c_void_p:
@@ -285,19 +294,10 @@ class KvCache:
             raise ValueError("cache was destroyed")
         return self._h
 
-    def pools(self, k_pages, v_pages):
-        """(pointer, pointer, pages) of the two pools."""
-        n = k_pages.shape[0]
-        if (k_pages.shape == (n, self.k_page_bytes) and v_pages.shape == (n, self.v_page_bytes) and k_pages.dtype is _torch.uint8 and v_pages.dtype is _torch.uint8
-                and k_pages.get_device() == self.device == v_pages.get_device() and k_pages.is_contiguous() and v_pages.is_contiguous()):
-            return k_pages.data_ptr(), v_pages.data_ptr(), n
-        raise ValueError(f"the pools are contiguous uint8 tensors [n_pages][{self.k_page_bytes}] and [n_pages][{self.v_page_bytes}] on the cache's device, got "
-                         f"{k_pages.dtype} {tuple(k_pages.shape)} and {v_pages.dtype} {tuple(v_pages.shape)}")
-
     def destroy(self) -> None:
         if getattr(self, "_h", None) is not None:
             _lib.rptq_kv_cache_destroy(self._h)
-            self._h = None
+            self._h = self._call = None
 
     def __del__(self):
         try:
@@ -306,47 +306,17 @@ class KvCache:
             pass
 
 
-def _cache_rows(cache: KvCache, k, v, n: int):
-    """Pointers, distances and type of the rows of K and V in a call with n tokens."""
-    kind, ks, vs, kt, vt, device = _rows_types.get(k.dtype), k.shape, v.shape, k.stride(), v.stride(), cache.device
-    ck, cv = (cache.k_row_bytes, cache.v_row_bytes) if kind == ROWS_CODES else (cache.C, cache.C)
-    if kind is None or v.dtype is not k.dtype:
-        raise ValueError(f"k and v have one type, fp32, fp16, bf16 or uint8 code rows: got {k.dtype} and {v.dtype}")
-    if (len(ks) != 2 or len(vs) != 2 or ks[0] < n or vs[0] < n or ks[1] < ck or vs[1] < cv or (kt[1] != 1 and ks[1] > 1) or (vt[1] != 1 and vs[1] > 1)
-            or k.get_device() != device or v.get_device() != device):
-        raise ValueError(f"k and v: expected at least {n} contiguous rows of {ck} and {cv} on the cache's device, got {tuple(ks)} and {tuple(vs)}")
-    return k.data_ptr(), kt[0] if ks[0] > 1 else ks[1], v.data_ptr(), vt[0] if vs[0] > 1 else vs[1], kind
-
-
-def _slots(cache: KvCache, slots):
-    """Pointer and number of a call's slots."""
-    shape = slots.shape
-    if slots.dtype is not _torch.int64 or len(shape) != 1 or slots.get_device() != cache.device or not slots.is_contiguous():
-        raise ValueError("slots: expected a contiguous 1-D tensor of int64 on the cache's device")
-    return slots.data_ptr(), shape[0]
-
-
 def kv_cache_write(cache: KvCache, k, v, slots, k_pages, v_pages, stream=None) -> None:
     """rptq_kv_cache_write: k, v [n][>= C] of fp16, bf16 or fp32 (original channel order; rows may lie apart, as in a slice of a fused
     projection's output), or uint8 code rows [n][>= row_bytes] of the layouts; slots int64 [n] (negative: skipped);
-    k_pages, v_pages uint8 [n_pages][page bytes]. CUDA tensors."""
-    at, n = _slots(cache, slots)
-    kp, vp, n_pages = cache.pools(k_pages, v_pages)
-    pk, ldk, pv, ldv, kind = _cache_rows(cache, k, v, n)
-    status = _lib.rptq_kv_cache_write(cache.handle, pk, ldk, pv, ldv, kind, at, n, kp, vp, n_pages, _stream_ptr(stream))
-    if status != OK:
-        raise RptqError(status, "rptq_kv_cache_write")
+    k_pages, v_pages uint8 [n_pages][page bytes]. CUDA tensors on the cache's device."""
+    _check(_calls.kv_cache_write(cache._call, k, v, slots, k_pages, v_pages, stream), "rptq_kv_cache_write")
 
 
 def kv_cache_read(cache: KvCache, k_pages, v_pages, slots, k_out, v_out, stream=None) -> None:
     """rptq_kv_cache_read: row i of k_out, v_out (fp16, bf16, fp32 [n][>= C], or uint8 code rows [n][>= row_bytes]) receives slot
     slots[i]; rows of negative slots stay as they are."""
-    at, n = _slots(cache, slots)
-    kp, vp, n_pages = cache.pools(k_pages, v_pages)
-    pk, ldk, pv, ldv, kind = _cache_rows(cache, k_out, v_out, n)
-    status = _lib.rptq_kv_cache_read(cache.handle, kp, vp, n_pages, at, n, pk, ldk, pv, ldv, kind, _stream_ptr(stream))
-    if status != OK:
-        raise RptqError(status, "rptq_kv_cache_read")
+    _check(_calls.kv_cache_read(cache._call, k_pages, v_pages, slots, k_out, v_out, stream), "rptq_kv_cache_read")
 
 
 def attention_paged_workspace_bytes(cache: KvCache, n_q_heads: Optional[int] = None) -> int:
@@ -365,30 +335,12 @@ def attention_paged(cache: KvCache, q, k_pages, v_pages, page_table, seq_lens, o
     """rptq_attention_paged: q, out fp16 or bf16 [n_seq][>= n_q_heads * d], page_table int32 [n_seq][pages], seq_lens int32 [n_seq]; CUDA
     tensors. n_q_heads: a multiple of the cache's heads (default: as many). workspace: a contiguous tensor of at least
     attention_paged_workspace_bytes(cache, n_q_heads) bytes, allocated by the call if None."""
-    if n_q_heads is None:
-        n_q_heads = cache.n_heads
-    device, dtype, cols = cache.device, q.dtype, n_q_heads * cache.head_dim
-    kind, qs, os, qt, ot, ls, ts, tt = _rows_types.get(dtype), q.shape, out.shape, q.stride(), out.stride(), seq_lens.shape, page_table.shape, page_table.stride()
-    n_seq = ls[0] if len(ls) == 1 else -1
-    if kind is None or out.dtype is not dtype:
-        raise ValueError(f"q and out have one type, fp16 or bf16: got {dtype} and {out.dtype}")
-    if (len(qs) != 2 or len(os) != 2 or qs[0] < n_seq or os[0] < n_seq or qs[1] < cols or os[1] < cols or (qt[1] != 1 and qs[1] > 1) or (ot[1] != 1 and os[1] > 1)
-            or q.get_device() != device or out.get_device() != device):
-        raise ValueError(f"q and out: expected at least {n_seq} contiguous rows of {cols} on the cache's device, got {tuple(qs)} and {tuple(os)}")
-    if (n_seq < 0 or len(ts) != 2 or ts[0] < n_seq or (tt[1] != 1 and ts[1] > 1) or seq_lens.dtype is not _torch.int32 or page_table.dtype is not _torch.int32
-            or seq_lens.get_device() != device or page_table.get_device() != device or not seq_lens.is_contiguous()):
-        raise ValueError(f"seq_lens [n_seq] and page_table [n_seq][pages] are int32 on the cache's device, got {seq_lens.dtype} {tuple(ls)} and {page_table.dtype} {tuple(ts)}")
-    kp, vp, n_pages = cache.pools(k_pages, v_pages)
+    n_q_heads = cache.n_heads if n_q_heads is None else n_q_heads
     need = attention_paged_workspace_bytes(cache, n_q_heads)
     if workspace is None:
-        workspace = _torch.empty(need, dtype=_torch.uint8, device=q.device)
-    elif workspace.nbytes < need or not workspace.is_contiguous() or workspace.get_device() != device:
-        raise ValueError(f"workspace: {need} contiguous bytes on the cache's device are needed")
-    status = _lib.rptq_attention_paged(cache.handle, q.data_ptr(), qt[0] if qs[0] > 1 else qs[1], kind, n_q_heads, n_seq, kp, vp, n_pages, page_table.data_ptr(),
-                                       tt[0] if ts[0] > 1 else ts[1], ts[1], seq_lens.data_ptr(), qk_scale, out.data_ptr(), ot[0] if os[0] > 1 else os[1],
-                                       workspace.data_ptr(), _stream_ptr(stream))
-    if status != OK:
-        raise RptqError(status, "rptq_attention_paged")
+        import torch
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    _check(_calls.attention_paged(cache._call, q, k_pages, v_pages, page_table, seq_lens, out, qk_scale, n_q_heads, workspace, need, stream), "rptq_attention_paged")
 
 
 def weight_pack(layout_in: Layout, W: np.ndarray, out_perm=None, n_pad: Optional[int] = None):

@@ -344,7 +344,7 @@ paged_kernel(const Params p)
 #pragma unroll
         for (int i = 0; i < UN; ++i) {
             const int ch = 32 * i + lane;
-            k_scale[i] = i < nu && n > 0 ? __ldg(&val[ch].x) : 0.f;
+            k_scale[i] = i < nu && n > 0 ? val[ch].x : 0.f;
             q_bits[i] = ch < p.d && n > 0 ? query_bits(p, of.s, h * p.G + q0, ch) : 0u;
             if (ch < p.d && n > 1) q_bits[i] |= (uint32_t)query_bits(p, of.s, h * p.G + q0 + 1, ch) << 16;
         }
@@ -665,7 +665,7 @@ paged_kernel(const Params p)
                 if (!mine || ch >= 32 * nu) continue;
                 float y[N];
 #pragma unroll
-                for (int i = 0; i < N; ++i) y[i] = complete ? result(o[N * x + i], l, inv, __ldg(val + ch + i)) : o[N * x + i];
+                for (int i = 0; i < N; ++i) y[i] = complete ? result(o[N * x + i], l, inv, val[ch + i]) : o[N * x + i];
                 if (complete) {
                     store_out<N>(p, c.s, head0 + q, ch, y);
                 } else {
@@ -713,7 +713,7 @@ paged_kernel(const Params p)
 #pragma unroll
             for (int x = 0; x < V; ++x)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) sz[x][k] = __ldg(val + min(4 * lane + 128 * x, 32 * nu - 4) + k);
+                for (int k = 0; k < 4; ++k) sz[x][k] = val[min(4 * lane + 128 * x, 32 * nu - 4) + k];
             l = 0.f;
 #pragma unroll
             for (int x = 0; x < V; ++x) o[x] = make_float4(0.f, 0.f, 0.f, 0.f);

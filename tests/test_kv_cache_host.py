@@ -99,3 +99,41 @@ def test_attention_refuses(binding):
     assert lib.rptq_attention_paged_workspace_bytes(cache.handle, 3) == inv
     with pytest.raises(binding.RptqError):
         binding.attention_paged_workspace_bytes(cache, 5)
+
+
+def test_tensors_that_do_not_fit_are_refused(binding):
+    """The marshalling in front of the library, on CPU tensors where there is no device (with one they are on the wrong device)."""
+    import torch
+    cache = binding.KvCache(_layout(binding, 128, 4), _layout(binding, 128, 3), 2, 16)
+    pools = [torch.zeros((3, b), dtype=torch.uint8) for b in (cache.k_page_bytes, cache.v_page_bytes)]
+    k, slots = torch.zeros((5, 130)), torch.zeros(5, dtype=torch.int64)
+    codes = [torch.zeros((5, b), dtype=torch.uint8) for b in (cache.k_row_bytes, cache.v_row_bytes)]
+    q, out = torch.zeros((4, 256), dtype=torch.float16), torch.zeros((4, 260), dtype=torch.float16)
+    table, lens, ws = torch.zeros((4, 2), dtype=torch.int32), torch.zeros(4, dtype=torch.int32), torch.zeros(64, dtype=torch.uint8)
+    cache._workspace[4] = 64                                                # (its size is the device's to say)
+    write = lambda *a, **kw: binding.kv_cache_write(cache, *a, **kw)
+    read = lambda *a, **kw: binding.kv_cache_read(cache, *a, **kw)
+    attend = lambda *a, **kw: binding.attention_paged(cache, *a, 0.1, n_q_heads=4, workspace=kw.pop("workspace", ws), **kw)
+    if not torch.cuda.is_available():
+        for call in (lambda: write(k, k, slots, *pools), lambda: write(k[:, 2:], k[:, 1:129], slots, *pools), lambda: write(*codes, slots, *pools),
+                     lambda: read(*pools, slots, k, k), lambda: read(*pools, slots[:2], *codes), lambda: attend(q, *pools, table, lens, out),
+                     lambda: attend(q[:1], *pools, table[:1, :1], lens[:1], out[:1, 4:])):
+            with pytest.raises(binding.RptqError) as e:                       # all arguments pass, a device is missing
+                call()
+            assert e.value.status == binding.ERR_CUDA
+    for call in (lambda: write(k, k, slots.int(), *pools), lambda: write(k, k, slots[::2], *pools), lambda: write(k[:4], k, slots, *pools),
+                 lambda: write(k[:, 3:], k, slots, *pools), lambda: write(k, k.half(), slots, *pools), lambda: write(k.double(), k.double(), slots, *pools),
+                 lambda: write(k.t(), k, slots, *pools), lambda: write(k[0], k[0], slots, *pools), lambda: write(codes[1], codes[0][:, 1:], slots, *pools),
+                 lambda: write(k, k, slots, pools[0], pools[1][:2]), lambda: write(k, k, slots, pools[1], pools[0]), lambda: write(k, None, slots, *pools),
+                 lambda: write(k, k, slots, pools[0].to(torch.int8), pools[1]), lambda: read(pools[0][:, ::2], pools[1], slots, k, k),
+                 lambda: read(*pools, slots, k[:, ::2], k), lambda: attend(q, *pools, table.long(), lens, out), lambda: attend(q, *pools, table, lens.long(), out),
+                 lambda: attend(q, *pools, table[:3], lens, out), lambda: attend(q, *pools, table, lens, out.float()), lambda: attend(q[:3], *pools, table, lens, out),
+                 lambda: attend(q[:, 1:], *pools, table, lens, out), lambda: attend(q, *pools, table, lens[None], out), lambda: attend(q, *pools, table[:, 0], lens, out),
+                 lambda: attend(q, *pools, table, lens, out, workspace=ws[:60]), lambda: attend(q, *pools, table, lens, out, workspace=ws.repeat(2)[::2])):
+        with pytest.raises(ValueError):
+            call()
+    cache.destroy()
+    with pytest.raises(ValueError):
+        write(k, k, slots, *pools)
+    with pytest.raises(ValueError):
+        attend(q, *pools, table, lens, out)
