@@ -53,7 +53,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if not force and not needs_build():
         return LIB
     tmp = LIB + f".tmp{os.getpid()}"
-    cmd = ["nvcc", "-shared", *NVCC_FLAGS, *(["-Xptxas", "-v"] if verbose else []),
+    cmd = ["nvcc", "-shared", "--threads", str(os.cpu_count() or 1), *NVCC_FLAGS, *(["-Xptxas", "-v"] if verbose else []),
            *sources(), "-o", tmp, "-lgomp"]
     subprocess.run(cmd, check=True)
     os.replace(tmp, LIB)
