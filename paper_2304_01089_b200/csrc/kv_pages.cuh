@@ -26,11 +26,12 @@ struct rptq_kv_cache {
     struct Tensor {
         int bits = 0, K_pad = 0;
         int64_t row_bytes = 0, slab_bytes = 0, page_bytes = 0;
-        float2* quant = nullptr;     // [H * 32 nu] {inv_s, bits of z - 0x4B400000}; pads give code 0
-        float2* value = nullptr;     // [H * 32 nu] {s, (float) z}
-        uint16_t* pos = nullptr;     // [C] position of the channel in a code row of the layout
-        int32_t* chan = nullptr;     // [K_pad] channel at the position, -1 at pads
+        const float2* quant = nullptr;     // [H * 32 nu] {inv_s, bits of z - 0x4B400000}; pads give code 0
+        const float2* value = nullptr;     // [H * 32 nu] {s, (float) z}
+        const uint16_t* pos = nullptr;     // [C] position of the channel in a code row of the layout
+        const int32_t* chan = nullptr;     // [K_pad] channel at the position, -1 at pads
     } k, v;
+    void* tables = nullptr;          // all of the device tables
 };
 
 namespace rptq {
