@@ -5,7 +5,7 @@ row's type, so numpy's fp32 product rounded the same way gives the same bits. At
 import numpy as np
 import pytest
 
-from paged_cases import Batch, Site, torch_dtype
+from paged_cases import HALF_STEP, Batch, Site, torch_dtype
 
 pytestmark = pytest.mark.gpu
 
@@ -327,6 +327,30 @@ def test_attention_queries_of_zero_and_of_extreme_size():
             b.q[:] = value
             b.q[0, 1] = 0.0
             b.check()
+
+
+def test_attention_scores_at_the_ends_of_their_range():
+    """Scores far below -2^99 are scores like others; those that could pass 2^127 are refused as a query that is not finite is."""
+    import torch
+    for G in (1, 4):
+        for bits in ((4, 4), (3, 3), (8, 8)):
+            b = Batch(585, 1, 64, bits, 16, [40, 1], G=G, dtype="bf16")
+            b.qk_scale = 1e30
+            for sign in (1.0, -1.0):
+                b.q[:] = sign
+                out = b.run().double().cpu().numpy().reshape(2, G, 64)
+                # the largest score is ahead of the others by far more than its rounding, and takes all: its value's row, rounded a few times
+                K, V = b.site.k.values(b.kq), b.site.v.values(b.vq)
+                S = 1e30 * sign * K[:40].sum(1)
+                order = np.argsort(S)
+                reach = 1e30 * np.abs(b.site.k.s.astype(np.float64)).sum() * ((1 << bits[0]) - 1)
+                assert np.abs(S).max() < 2.0 ** 126 and S[order[-1]] - S[order[-2]] > 72 * 2.0 ** -24 * 1.4427 * reach + 1000
+                reach_v = np.abs(b.site.v.s) * (np.abs(b.site.v.z) + (1 << bits[1]))
+                for i, row in enumerate((V[order[-1]], V[40])):
+                    assert (np.abs(out[i] - row) <= HALF_STEP["bf16"] * np.abs(row) + 8 * 2.0 ** -24 * reach_v).all()
+            b.q[:, 0] = 1e38
+            out = b.run()
+            assert bool(torch.isnan(out[:, :64]).all()) and bool(torch.isfinite(out[:, 64:]).all())
 
 
 def test_attention_is_the_same_every_time():
