@@ -2,7 +2,8 @@
 
 Every step of the hot path runs in the library's CUDA kernels. PyTorch appears here only as the
 owner of device memory and streams. If the library is missing this module raises at import time;
-there is no fallback path.
+there is no fallback path. The paged cache's calls hand their tensors over through _calls.so
+(csrc/calls.cpp), the others through ctypes.
 """
 from __future__ import annotations
 
