@@ -340,7 +340,9 @@ def attention_paged(cache: KvCache, q, k_pages, v_pages, page_table, seq_lens, o
     need = attention_paged_workspace_bytes(cache, n_q_heads)
     if workspace is None:
         import torch
-        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+        on = stream if stream is None or hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream))
+        with torch.cuda.stream(on):                        # its memory is used again on the stream that the call runs on, and on no other
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
     _check(_calls.attention_paged(cache._call, q, k_pages, v_pages, page_table, seq_lens, out, qk_scale, n_q_heads, workspace, need, stream), "rptq_attention_paged")
 
 

@@ -451,6 +451,89 @@ def test_on_other_streams_and_in_a_graph():
     assert binding.get_device_status() == 0
 
 
+@pytest.mark.parametrize("as_number", [False, True])
+def test_a_workspace_that_the_call_allocates_belongs_to_its_stream(as_number, monkeypatch):
+    """While the call waits on its stream, the current stream is not handed the memory of its workspace."""
+    import torch
+    from paper_2304_01089_b200 import binding
+    b = Batch(623, 2, 128, (4, 4), 16, [5000, 70])
+    want = b.check()
+    need = binding.attention_paged_workspace_bytes(b.site.cache)
+    at = []
+
+    class Seen:
+        def attention_paged(self, *args):
+            at.append(args[9].data_ptr())
+            return real.attention_paged(*args)
+
+    real, side, out = binding._calls, torch.cuda.Stream(), torch.empty_like(b.q)
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    monkeypatch.setattr(binding, "_calls", Seen())
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(20_000_000)
+    binding.attention_paged(b.site.cache, b.q, *b.pools, b.table_dev, b.lens_dev, out, b.qk_scale, stream=side.cuda_stream if as_number else side)
+    mine = [torch.empty(need, dtype=torch.uint8, device="cuda").random_(0, 256) for _ in range(4)]
+    assert at and not any(m.data_ptr() <= at[0] < m.data_ptr() + need or at[0] <= m.data_ptr() < at[0] + need for m in mine)
+    torch.cuda.synchronize()
+    assert torch.equal(out, want)
+
+
+def test_tables_of_no_pages():
+    import torch
+    from paper_2304_01089_b200 import binding
+    b = Batch(624, 2, 64, (4, 4), 16, [20, 3])
+    out = torch.full_like(b.q, float("nan"))
+    binding.attention_paged(b.site.cache, b.q, *b.pools, b.table_dev[:, :0].contiguous(), b.lens_dev, out, b.qk_scale)
+    assert not bool(out.any())
+    assert binding.get_device_status() == 0
+
+
+_FIRST = """
+import numpy as np, torch
+from paged_cases import Site
+from paper_2304_01089_b200 import binding
+s = Site(628, 2, 64, {bits}, 16)
+pools = s.pools(30)
+k, v = (torch.randn((450, s.C), dtype=torch.float16, device="cuda") for _ in range(2))
+slots = torch.arange(450, device="cuda")
+q = torch.randn((2, s.C * {G}), dtype=torch.float16, device="cuda")
+table = torch.arange(30, dtype=torch.int32, device="cuda").reshape(2, 15)
+lens = torch.tensor([240, 200], dtype=torch.int32, device="cuda")
+out = [torch.zeros_like(q) for _ in range(2)]
+back = [[torch.zeros_like(k) for _ in range(2)] for _ in range(2)]
+ws = torch.empty(binding.attention_paged_workspace_bytes(s.cache, 2 * {G}), dtype=torch.uint8, device="cuda")
+def call(i):
+    binding.kv_cache_write(s.cache, k, v, slots, *pools)
+    binding.kv_cache_read(s.cache, *pools, slots, *back[i])
+    binding.attention_paged(s.cache, q, *pools, table, lens, out[i], 0.125, n_q_heads=2 * {G}, workspace=ws)
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    call(0)
+for p in pools:
+    p.zero_()
+graph.replay()
+torch.cuda.synchronize()
+call(1)
+torch.cuda.synchronize()
+assert bool(out[1].any()) and torch.equal(out[0], out[1])
+assert all(bool(y.any()) and torch.equal(x, y) for x, y in zip(*back))
+assert binding.get_device_status() == 0
+print("same")
+"""
+
+
+@pytest.mark.parametrize("bits, G", [((4, 4), 1), ((3, 8), 4)])
+def test_first_calls_of_a_process_can_be_captured(bits, G):
+    import os
+    import subprocess
+    import sys
+    here = os.path.dirname(os.path.abspath(__file__))
+    env = dict(os.environ, PYTHONPATH=os.pathsep.join([here, os.path.dirname(here), os.environ.get("PYTHONPATH", "")]))
+    r = subprocess.run([sys.executable, "-c", _FIRST.format(bits=bits, G=G)], capture_output=True, text=True, timeout=300, env=env)
+    assert r.returncode == 0 and r.stdout.split()[-1:] == ["same"], r.stderr[-2000:]
+
+
 def test_two_graphs_that_share_a_workspace():
     """Captured over the same workspace and replayed by turns, with other work over it in between: what a call finds there does not matter."""
     import torch
