@@ -4,6 +4,8 @@ from __future__ import annotations
 import numpy as np
 
 HALF_STEP = {"f16": 2.0 ** -11, "bf16": 2.0 ** -8, "f32": 2.0 ** -24}
+# Relative to a number of at least this size; below it the steps stay as they are at it (fp16: 2^-24 apart, so a rounding is off by up to 2^-25)
+SMALLEST_NORMAL = {"f16": 2.0 ** -14, "bf16": 2.0 ** -126, "f32": 2.0 ** -126}
 
 
 def torch_dtype(name):
@@ -144,7 +146,7 @@ class Batch:
             reach = np.abs(s.v.s.astype(np.float64)).reshape(1, s.H, d) * np.maximum(vq, np.abs(vq - s.v.z)).reshape(n, s.H, d)   # codes and values
             mass = np.einsum("hgn,nhd->hgd", P + 2.0 ** -25 / total, reach)
             bound[i] = (2 * E + (n + 8) * 2.0 ** -24) * mass + 2 * n * 2.0 ** -25 / total * reach.max(0)[:, None, :] + 1e-30
-        bound += HALF_STEP[self.dtype] * (np.abs(out) + bound)
+        bound += HALF_STEP[self.dtype] * np.maximum(np.abs(out) + bound, SMALLEST_NORMAL[self.dtype])
         return out.reshape(len(self.lens), -1), bound.reshape(len(self.lens), -1)
 
     def check(self, **kw):
