@@ -14,7 +14,7 @@ constexpr int MIN_SHARE = PAIR_COST + 2;       // least share of a group
 constexpr int WHOLE_TILES = 4;                 // pairs of at most so many tiles are not split
 
 // How a cache is worked on with G query heads per cached head: the instance knows its sizes (`exact`), warps of a group, blocks per SM.
-struct Plan { bool exact; int un, warps, chunks, smem, blocks_per_sm; };
+struct Plan { bool exact; int un, warps, chunks, smem, blocks; };
 static Plan plan_of(const rptq_kv_cache_t* c, int G)
 {
     Plan x{};
@@ -24,7 +24,7 @@ static Plan plan_of(const rptq_kv_cache_t* c, int G)
     x.chunks = (G + x.warps * WARP_Q - 1) / (x.warps * WARP_Q);
     x.smem = WARPS / x.warps * STAGES * stage_bytes(c->k.bits, c->v.bits, c->nu) + WARPS * scratch_bytes(c->k.bits, x.un);
     const int by_smem = (SMEM_MAX + 1024) / (x.smem + 1024);
-    x.blocks_per_sm = by_smem < BLOCKS_PER_SM ? by_smem : BLOCKS_PER_SM;
+    x.blocks = by_smem < blocks_per_sm(x.un) ? by_smem : blocks_per_sm(x.un);
     return x;
 }
 
@@ -48,7 +48,7 @@ int64_t rptq_attention_paged_workspace_bytes(const rptq_kv_cache_t* cache, int n
     const int n_sm = cache->device < 0 ? 0 : sm_count(cache->device);
     if (n_sm == 0) return RPTQ_ERR_CUDA;
     const Plan x = plan_of(cache, n_q_heads / cache->H);
-    return (int64_t)n_sm * x.blocks_per_sm * WARPS * (3 * 8 + 2 * WARP_Q * 4 * part_pitch(cache->nu));
+    return (int64_t)n_sm * x.blocks * WARPS * (3 * 8 + 2 * WARP_Q * 4 * part_pitch(cache->nu));
 }
 
 int rptq_attention_paged(const rptq_kv_cache_t* cache, const void* q, int64_t ldq, int q_type, int n_q_heads, int n_seq,
@@ -94,7 +94,7 @@ int rptq_attention_paged(const rptq_kv_cache_t* cache, const void* q, int64_t ld
     p.mark = process_mark();
     p.status = device_status_word();
     p.warps = x.warps;
-    const int64_t most = (int64_t)n_sm * x.blocks_per_sm;
+    const int64_t most = (int64_t)n_sm * x.blocks;
     p.parts = reinterpret_cast<float*>(p.arrived + 3 * most * WARPS);
 
     // a grid that fills the GPU is the most

@@ -58,7 +58,9 @@ constexpr int FLUSH_TILES = 1000;              // 32 keys x 255 x 255 a tile sta
 
 constexpr int SMEM_MAX = 227 * 1024;           // of a block
 constexpr int STAGES = 2;                      // of a group's ring. (Three, more of the cache under way: 2 to 4 % slower; four: 5 %)
-constexpr int BLOCKS_PER_SM = 3;               // 168 registers a thread. (Four, 128: 4 to 17 % slower; two: up to 12 %)
+// 168 registers a thread. (Four, 128: 4 to 17 % slower; two: up to 12 %.) Heads of more than 128 channels need up to 255: with 168 they spill, 32
+// sequences of up to 3000 keys, 16 heads of 256 channels, 4 bits, took 60.5 us with three blocks, 45.0 with two; 8 bits, 8 heads for 32, 65.9 and 45.4.
+__host__ __device__ constexpr int blocks_per_sm(int un) { return un <= 4 ? 3 : 2; }
 // bytes of a stage of a ring: two slabs of each tensor
 __host__ __device__ constexpr int stage_bytes(int bits_k, int bits_v, int nu) { return 2 * SLAB * 4 * nu * (bits_k + bits_v); }
 // a warp's own: the staged query of one head, or the tile's probabilities
@@ -211,7 +213,7 @@ __device__ __forceinline__ void store_out(const Params& p, int s, int head, int 
 
 // BK, BV: bits of the keys' and the values' codes; UN: units of 32 channels a head may have (EXACT: has); R: warps of a group (0: p.warps).
 template <int BK, int BV, int UN, bool EXACT, int R>
-__global__ void __launch_bounds__(THREADS, BLOCKS_PER_SM)
+__global__ void __launch_bounds__(THREADS, blocks_per_sm(UN))
 paged_kernel(const Params p)
 {
     constexpr int KQ = BK == 8 ? (UN + 1) / 2 : (UN + 3) / 4, KI = BK == 8 ? 2 : BK == 4 ? 4 : 5;      // groups of four 16-byte pieces, products per group
