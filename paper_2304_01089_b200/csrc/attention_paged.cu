@@ -18,7 +18,7 @@ struct Plan { bool exact; int un, warps, chunks, smem, blocks; };
 static Plan plan_of(const rptq_kv_cache_t* c, int G)
 {
     Plan x{};
-    x.exact = c->k.bits == c->v.bits && (c->nu == 8 || (c->nu >= 2 && c->nu <= 4));
+    x.exact = c->nu == 8 || (c->nu >= 2 && c->nu <= 4);
     x.un = x.exact ? c->nu : c->nu <= 4 ? 4 : 8;
     x.warps = G <= WARP_Q ? 1 : G <= 2 * WARP_Q ? 2 : 4;
     x.chunks = (G + x.warps * WARP_Q - 1) / (x.warps * WARP_Q);

@@ -26,16 +26,15 @@ int launch_exact(const Params& p, const Launch& l)
 {
     return p.warps == 1 ? launch_one<BK, BV, UN, true, 1>(p, l) : p.warps == 2 ? launch_one<BK, BV, UN, true, 2>(p, l) : launch_one<BK, BV, UN, true, 4>(p, l);
 }
-// The common sizes of heads in a cache whose tensors have the same bits know their sizes when they are compiled.
+// The common sizes of heads are known when the instance is compiled, which saves 10 to 20 % (16 sequences of up to 3000 keys, keys of 8 and values
+// of 4 bits, 32 heads of 128 channels: 33.0 -> 29.4 us; 8 cached heads for 32: 21.2 -> 18.5).
 template <int BK, int BV>
 int launch_size(const Params& p, const Launch& l)
 {
-    if constexpr (BK == BV) {
-        if (p.nu == 2) return launch_exact<BK, BV, 2>(p, l);
-        if (p.nu == 3) return launch_exact<BK, BV, 3>(p, l);
-        if (p.nu == 4) return launch_exact<BK, BV, 4>(p, l);
-        if (p.nu == 8) return launch_exact<BK, BV, 8>(p, l);
-    }
+    if (p.nu == 2) return launch_exact<BK, BV, 2>(p, l);
+    if (p.nu == 3) return launch_exact<BK, BV, 3>(p, l);
+    if (p.nu == 4) return launch_exact<BK, BV, 4>(p, l);
+    if (p.nu == 8) return launch_exact<BK, BV, 8>(p, l);
     return l.un == 4 ? launch_one<BK, BV, 4, false, 0>(p, l) : launch_one<BK, BV, 8, false, 0>(p, l);
 }
 template <int BK>
