@@ -11,7 +11,6 @@ namespace attn_paged {
 
 constexpr int MAX_KEYS = 1 << 30;              // per sequence
 constexpr int MIN_SHARE = PAIR_COST + 2;       // least share of a group
-constexpr int WHOLE_TILES = 4;                 // pairs of at most so many tiles are not split
 
 // How a cache is worked on with G query heads per cached head: the instance knows its sizes (`exact`), warps of a group, blocks per SM.
 struct Plan { bool exact; int un, warps, chunks, smem, blocks; };
@@ -98,7 +97,7 @@ int rptq_attention_paged(const rptq_kv_cache_t* cache, const void* q, int64_t ld
     p.parts = reinterpret_cast<float*>(p.arrived + 3 * most * WARPS);
 
     // a grid that fills the GPU is the most
-    p.whole = max_tiles <= WHOLE_TILES;
+    p.whole = max_tiles <= FEW_TILES;
     p.min_share = MIN_SHARE;
     const int64_t groups = p.whole ? all_pairs : (all_pairs * (max_tiles + PAIR_COST) + MIN_SHARE - 1) / MIN_SHARE;
     Launch l{};

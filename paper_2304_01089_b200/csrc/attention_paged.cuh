@@ -49,6 +49,11 @@ constexpr int TILE = 2 * SLAB;                 // keys
 constexpr int WARPS = 4, THREADS = 32 * WARPS;  // of a block: 4, 2 or 1 groups
 constexpr int PAIR_COST = 4;                   // tiles that beginning and ending a pair counts as
 constexpr int WARP_Q = 2;                      // query heads of a warp
+constexpr int FEW_TILES = 4;                   // pairs of at most so many tiles are not split, nor
+constexpr int WHOLE_TILES = 10;                // those of at most so many where every pair can have a group of its own: splitting and joining costs about
+                                               // as much as six tiles. (4 sequences of 130 keys, 8 cached heads of 128 for 32, 4 bits: 12.4 us split, 7.2
+                                               // whole; of 330 keys 11.6 and 11.2. 64 sequences of 330 keys, 32 heads, more pairs than groups: 18.5 and 23.2.
+                                               // The groups decide, because only they know the lengths: long calls pay 0.3 to 0.6 us for it)
 constexpr int MANY_PARTS = 32;                 // more parts of a pair than these are joined in two levels
 constexpr int MAX_TRIES = 1 << 14;             // (every failed one is another group's success, of which there are a few per part)
 constexpr float HEAD = 4.0f;                   // how far above the largest score a moved reference lies, in powers of two
@@ -78,7 +83,7 @@ struct Params {
     int n_seq, H, G, d, nu, P, max_len;
     int chunks;                                // sets of WARP_Q * warps query heads per cached head
     int warps;                                 // of a group
-    int whole;                                 // a group takes whole pairs, every n-th; nothing is split
+    int whole;                                 // the table has room for FEW_TILES a pair at most
     int min_share;                             // least share of a group
     float scale_log2e;
     // [groups][3][warps] parts that are there, under the process's mark: of the run of parts that begins with the group's part of the pair which
@@ -99,16 +104,20 @@ struct Cursor {
     bool ok;
 };
 
-// All lanes: a group's share of the list, and the list's length. (The host sees to it that the list and its places stay below 2^31.)
+// All lanes: a group's share of the list (0: groups take whole pairs), and the list's length. (The host sees to it that the list and its
+// places stay below 2^31.)
 __device__ __forceinline__ int find_shares(const Params& p, int pairs, int n_groups, int& share)
 {
+    const int whole = p.n_seq * pairs <= n_groups ? WHOLE_TILES : FEW_TILES;
     int n = 0;
+    bool split = false;
     for (int s = threadIdx.x & 31; s < p.n_seq; s += 32) {
         const int nt = tiles_of(len_of(p, s));
         n += nt > 0 ? nt + PAIR_COST : 0;
+        split |= nt > whole;
     }
     const int total = __reduce_add_sync(0xffffffffu, n) * pairs;
-    share = max((total + n_groups - 1) / n_groups, p.min_share);
+    share = __any_sync(0xffffffffu, split) ? max((total + n_groups - 1) / n_groups, p.min_share) : 0;
     return total;
 }
 // My tiles of the pair c.s, c.pair, which begins at c.begin: those at places first .. end - 1 of the list.
@@ -164,9 +173,9 @@ __device__ __forceinline__ void find_pair(const Params& p, int pairs, int step, 
     c.ok = false;
 }
 // From the end of my part of a pair to the next pair; `end`: of my share.
-__device__ __forceinline__ void next_pair(const Params& p, int pairs, int step, int end, Cursor& c)
+__device__ __forceinline__ void next_pair(const Params& p, int pairs, bool whole, int step, int end, Cursor& c)
 {
-    if (p.whole) { c.begin += step; find_pair(p, pairs, step, c); return; }
+    if (whole) { c.begin += step; find_pair(p, pairs, step, c); return; }
     c.begin += c.nt + PAIR_COST;
     if (c.begin >= end) { c.ok = false; return; }
     if (++c.pair == pairs) {
@@ -247,16 +256,16 @@ paged_kernel(const Params p)
 
     Cursor in{};                                           // what is loaded next
     int share = 0, end = 0;
-    if (p.whole) {
-        in.ok = true;
-        in.begin = me;
-        find_pair(p, pairs, n_groups, in);
-    } else {
-        const int total = find_shares(p, pairs, n_groups, share);
+    const int total = p.whole ? 0 : find_shares(p, pairs, n_groups, share);
+    if (share > 0) {
         if (me <= (total - 1) / share) {
             end = min(me * share + share, total);
             find_tile(p, pairs, me * share, end, in);
         }
+    } else {
+        in.ok = true;
+        in.begin = me;
+        find_pair(p, pairs, n_groups, in);
     }
     if (!in.ok) return;
     Cursor c = in;                                         // what is worked on
@@ -322,7 +331,7 @@ paged_kernel(const Params p)
             if ((missing & 3u) && p.status) *p.status = RPTQ_ERR_BAD_SLOT;
             ++in.t;
             if (--in.n == 0) {
-                next_pair(p, pairs, n_groups, end, in);
+                next_pair(p, pairs, share == 0, n_groups, end, in);
                 if (in.ok) seek();
             }
         }
@@ -790,7 +799,7 @@ paged_kernel(const Params p)
         begins = --c.n == 0;                                   // of the next pair
         if (begins) {
             Cursor next = c;
-            next_pair(p, pairs, n_groups, end, next);
+            next_pair(p, pairs, share == 0, n_groups, end, next);
             if (next.ok) load_query(next);
         }
         if (R == 1 || n_heads > 0) work(ring + out_stage * stage, ring + out_stage * stage + 2 * k_slab);
@@ -798,7 +807,7 @@ paged_kernel(const Params p)
         ++c.t;
         if (begins) {
             if (R == 1 || n_heads > 0) finish();
-            next_pair(p, pairs, n_groups, end, c);
+            next_pair(p, pairs, share == 0, n_groups, end, c);
             first_t = 0;
         }
     }
