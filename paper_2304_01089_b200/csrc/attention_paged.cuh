@@ -24,8 +24,8 @@
 //     columns took three instructions per four codes to convert, twice the registers, and 50 us where this takes 24 us: 64 sequences of
 //     up to 1337 keys, 32 query heads on 8 cached ones, 8 bits.)
 // Measured: 72 heads of 128 channels, eight sequences of up to 2011 keys (10904 in all), 4 bits: 24.5 us, of which finding the share, the
-// first tiles, parts and join take 8 and the rest runs at 5.8 TB/s; one sequence of 65553 keys, 32 heads: 53 us, 5.1 TB/s over all; 3 bits, 96
-// heads, sixteen sequences of up to 1700 keys: 35.5 us, 3.2 TB/s, where instructions bound it too.
+// first tiles, parts and join take 8 and the rest runs at 5.8 TB/s; one sequence of 65553 keys, 32 heads: 52.5 us, 5.1 TB/s over all; 3 bits, 96
+// heads, sixteen sequences of up to 1700 keys: 35.2 us, 3.2 TB/s, where instructions bound it too.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
