@@ -758,6 +758,7 @@ paged_kernel(const Params p)
                     }
                     if (++i < count) continue;
                     float* sum = part_of(g_first + from, from == 0, head);
+                    __syncwarp();                                              // every lane has read the first part's reference and sum, which lane 0 replaces
                     if (level == 0 && lane == 0) *reinterpret_cast<float2*>(sum) = make_float2(top, l);
                     const float to_one = 1.0f / l;
 #pragma unroll

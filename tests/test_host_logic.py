@@ -362,3 +362,16 @@ def test_waits_of_whole_warps_are_voted(name):
         else:
             assert any(a < m.start() < b for a, b in one_lane), text[m.start() - 60:m.end() + 60]
     assert voted > 0
+
+
+def test_a_run_of_parts_is_read_by_all_lanes_before_its_sum_replaces_the_first():
+    """Paged attention joins many parts in runs, and a run's reference and sum are stored by one lane where all lanes have just loaded those of
+    its first part: without a synchronisation of the warp in between a lane that lags could add the run's sum in the part's place. No
+    run shows that while the warp happens to stay together, so the source is read."""
+    text = re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, "attention_paged.cuh")).read())
+    join = text[text.index("const int all = count * n_heads;"):]
+    load = join.index("__ldcg(reinterpret_cast<const float2*>(at))")
+    store = join.index("*reinterpret_cast<float2*>(sum) =")
+    assert load < join.index("__syncwarp();", load) < store
+    branch = join[:store].rindex("if (++i < count) continue;")             # uniform: every lane comes to the synchronisation
+    assert branch < join.index("__syncwarp();", load)
