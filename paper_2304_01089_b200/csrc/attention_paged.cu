@@ -81,7 +81,7 @@ int rptq_attention_paged(const rptq_kv_cache_t* cache, const void* q, int64_t ld
     p.k = static_cast<const uint8_t*>(k_pages); p.v = static_cast<const uint8_t*>(v_pages);
     p.k_page = (uint32_t)cache->k.page_bytes; p.v_page = (uint32_t)cache->v.page_bytes;
     p.n_pages = (uint32_t)(n_pages < INT_MAX ? n_pages : INT_MAX);          // (a page number is an int32)
-    p.val_k = cache->k.value; p.val_v = cache->v.value;
+    p.val_k = cache->k.value; p.val_v = cache->v.rest; p.centre_v = cache->v.centre;
     p.q = q; p.ldq = ldq; p.out = out; p.ldo = ldo; p.bf16 = q_type == RPTQ_ROWS_BF16;
     p.vector_out = aligned16(out) && ldo % 8 == 0 && cache->d % 8 == 0;
     p.table = page_table; p.ld_table = ld_table; p.lens = seq_lens;

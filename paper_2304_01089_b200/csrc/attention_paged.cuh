@@ -68,14 +68,16 @@ constexpr int STAGES = 2;                      // of a group's ring. (Three, mor
 __host__ __device__ constexpr int blocks_per_sm(int un) { return un <= 4 ? 3 : 2; }
 // bytes of a stage of a ring: two slabs of each tensor
 __host__ __device__ constexpr int stage_bytes(int bits_k, int bits_v, int nu) { return 2 * SLAB * 4 * nu * (bits_k + bits_v); }
-// a warp's own: the staged query of one head, or the tile's probabilities
+// a warp's own: the staged query of one head, or the tile's probabilities; behind them V's zero points of the pair's head, a byte each
 __host__ __device__ constexpr int unit_pitch(int bits_k) { return bits_k == 3 ? 44 : 36; }       // words between the units of the staged query: the
                                                                  // four pieces of a row group in different banks
-__host__ __device__ constexpr int scratch_bytes(int bits_k, int un) { return un * unit_pitch(bits_k) * 4 > WARP_Q * TILE * 4 ? un * unit_pitch(bits_k) * 4 : WARP_Q * TILE * 4; }
+__host__ __device__ constexpr int zeros_at(int bits_k, int un) { return un * unit_pitch(bits_k) * 4 > WARP_Q * TILE * 4 ? un * unit_pitch(bits_k) * 4 : WARP_Q * TILE * 4; }
+__host__ __device__ constexpr int scratch_bytes(int bits_k, int un) { return zeros_at(bits_k, un) + (un + 3) / 4 * 128; }
 __host__ __device__ constexpr int part_pitch(int nu) { return 4 + 32 * nu; }
 struct Params {
     const uint8_t *k, *v;
-    const float2 *val_k, *val_v;
+    const float2 *val_k, *val_v;               // [H * 32 nu] K's {s, z}; V's {s, z - centre}
+    const uint8_t* centre_v;                   // [H * 32 nu] V's zero points, or the codes nearest to them
     const void* q; int64_t ldq; void* out; int64_t ldo; int bf16, vector_out;
     const int32_t* table; int64_t ld_table;
     const int32_t* lens;
@@ -353,9 +355,12 @@ paged_kernel(const Params p)
     // my channels 32 i + lane of the query heads and of K's scales, loaded a tile before they are used
     uint32_t q_bits[UN];
     float k_scale[UN];
+    uint32_t zero_words[(UN + 3) / 4];                     // of channels 128 i + 4 lane ..
     auto load_query = [&](const Cursor& of) {
         const int h = of.pair / p.chunks, q0 = (of.pair - h * p.chunks) * (WARP_Q * warps) + WARP_Q * warp, n = p.G - q0;
         const float2* val = p.val_k + (int64_t)h * nu * 32;
+#pragma unroll
+        for (int i = 0; i < UN; i += 4) zero_words[i / 4] = 32 * i + 4 * lane < 32 * nu ? *reinterpret_cast<const uint32_t*>(p.centre_v + h * nu * 32 + 32 * i + 4 * lane) : 0u;
 #pragma unroll
         for (int i = 0; i < UN; ++i) {
             const int ch = 32 * i + lane;
@@ -364,6 +369,7 @@ paged_kernel(const Params p)
             if (ch < p.d && n > 1) q_bits[i] |= (uint32_t)query_bits(p, of.s, h * p.G + q0 + 1, ch) << 16;
         }
     };
+    uint8_t* const zeros = reinterpret_cast<uint8_t*>(scratch) + zeros_at(BK, UN);
     auto start_pair = [&]() {
         n_heads = min(WARP_Q, p.G - (c.pair % p.chunks) * (WARP_Q * warps) - WARP_Q * warp);
         if (n_heads <= 0) return;
@@ -455,6 +461,8 @@ paged_kernel(const Params p)
                     }
                 }
         }
+#pragma unroll
+        for (int i = 0; i < UN; i += 4) *reinterpret_cast<uint32_t*>(zeros + 32 * i + 4 * lane) = zero_words[i / 4];
         __syncwarp();
         ref = NO_REF;
 #pragma unroll
@@ -471,6 +479,8 @@ paged_kernel(const Params p)
         since = 0;
     };
     // The integers move into the 32-bit floating sums, times f. The two digits are joined in floating point: a sum may have 31 bits.
+    // The floating sums are of code - zero point (of one outside the codes: less the nearest code), the subtraction still exact: in sums of the
+    // codes the outputs, which are means of values around zero, would be differences of far larger numbers.
     auto flush = [&](float f) {
         const float w0 = weight, w1 = 256.0f * weight;
         if constexpr (BV == 3) {
@@ -478,6 +488,8 @@ paged_kernel(const Params p)
             // single bits on top
 #pragma unroll
             for (int j = 0; j < NB / 2; ++j) {
+                const uint4 zs = *reinterpret_cast<const uint4*>(zeros + 128 * j + 16 * g8);
+                const uint32_t z[4] = {zs.x, zs.y, zs.z, zs.w};
                 int v[2][16];
 #pragma unroll
                 for (int d = 0; d < 2; ++d) {
@@ -497,16 +509,29 @@ paged_kernel(const Params p)
                     }
                 }
 #pragma unroll
+                for (int n = 0; n < 16; ++n)
+#pragma unroll
+                    for (int d = 0; d < 2; ++d) v[d][n] -= (int)((z[n >> 2] >> (8 * (n & 3))) & 255u) * L[d];
+#pragma unroll
                 for (int n = 0; n < 16; ++n) {
                     float& x = F[2 * j + (n >> 3)][n & 3][(n >> 2) & 1];
                     x = f * (x + __fmaf_rn(w1, (float)v[1][n], w0 * (float)v[0][n]));
                 }
             }
         } else {
+            uint2 z = make_uint2(0u, 0u);
 #pragma unroll
             for (int m = 0; m < NM; ++m) {
+                if (!EXACT && 2 * (m >> 2) >= nu) break;
+                if (BV == 8 && m % 2 == 0) z.x = *reinterpret_cast<const uint32_t*>(zeros + 32 * (m >> 1) + 4 * g8);
+                if (BV == 4 && m % 4 == 0) z = *reinterpret_cast<const uint2*>(zeros + 64 * (m >> 2) + 8 * g8);
                 int (&o)[4] = O[m];
                 if constexpr (RAW) { o[2] -= o[0]; o[3] -= o[1]; }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t word = BV == 4 && i >= 2 ? z.y : z.x, byte = BV == 8 ? 2 * (m & 1) + (i >> 1) : m & 3;
+                    o[i] -= (int)((word >> (8 * byte)) & 255u) * (BV == 4 && i >= 2 ? 16 * L[i & 1] : L[i & 1]);
+                }
 #pragma unroll
                 for (int r = 0; r < 2; ++r) F[m >> 2][m & 3][r] = f * (F[m >> 2][m & 3][r] + __fmaf_rn(w1, (float)o[2 * r + 1], w0 * (float)o[2 * r]));
             }
@@ -520,7 +545,7 @@ paged_kernel(const Params p)
         for (int i = 0; i < 4; ++i) L[i] = 0;
         since = 0;
     };
-    // What the join and the direct end of a pair have in common: o / l with V's parameters.
+    // What the join and the direct end of a pair have in common: o / l with V's parameters, the zero point but for what the sums have lost of it.
     auto result = [&](float o, float l, float inv, float2 sz) { return l == 0.f ? 0.f : sz.x * (o * inv - sz.y); };
 
     // One tile.
@@ -584,7 +609,7 @@ paged_kernel(const Params p)
 #pragma unroll
             for (int o = 4; o < 32; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
             const float to = m > ref ? ceilf(m) + HEAD : ref;
-            flush(ex2(fmaxf(ref - to, -1000.0f)));
+            if (since > 0) flush(ex2(fmaxf(ref - to, -1000.0f)));             // (nothing is there at a pair's first tile)
             ref = to;
         }
         ++since;

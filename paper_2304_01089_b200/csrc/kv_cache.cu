@@ -11,6 +11,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <algorithm>
 #include <climits>
 #include <cstring>
 #include <new>
@@ -593,7 +594,7 @@ struct Tables {
         return at;
     }
 };
-struct TensorTables { size_t quant, value, pos, chan; };
+struct TensorTables { size_t quant, value, centre, rest, pos, chan; };
 
 static TensorTables make_tensor(const rptq_layout_t* L, const rptq_kv_cache& c, rptq_kv_cache::Tensor& t, Tables& tables)
 {
@@ -601,7 +602,8 @@ static TensorTables make_tensor(const rptq_layout_t* L, const rptq_kv_cache& c, 
     t.slab_bytes = (int64_t)SLAB * c.nu * 4 * L->bits;
     t.page_bytes = t.slab_bytes * (c.P / SLAB) * c.H;
     const size_t n = (size_t)c.H * c.nu * 32;
-    std::vector<float2> quant(n), value(n, make_float2(0.f, 0.f));
+    std::vector<float2> quant(n), value(n, make_float2(0.f, 0.f)), rest(value);
+    std::vector<uint8_t> centre(n, 0);
     std::vector<uint16_t> pos((size_t)c.C);
     std::vector<int32_t> chan((size_t)L->K_pad, -1);
     const int32_t magic = -0x4B400000;                       // pads: 0 * 0 rounds to 0, code 0
@@ -615,15 +617,19 @@ static TensorTables make_tensor(const rptq_layout_t* L, const rptq_kv_cache& c, 
             quant[at].x = (float)(1.0 / (double)L->scale[(size_t)cl]);
             std::memcpy(&quant[at].y, &zc, 4);
             value[at] = make_float2(L->scale[(size_t)cl], (float)L->zero[(size_t)cl]);
+            centre[at] = (uint8_t)std::min(std::max(L->zero[(size_t)cl], 0), (1 << L->bits) - 1);
+            rest[at] = make_float2(L->scale[(size_t)cl], (float)(L->zero[(size_t)cl] - centre[at]));
             pos[(size_t)ch] = (uint16_t)L->pos[j];
             chan[(size_t)L->pos[j]] = ch;
         }
-    return {tables.add(quant), tables.add(value), tables.add(pos), tables.add(chan)};
+    return {tables.add(quant), tables.add(value), tables.add(centre), tables.add(rest), tables.add(pos), tables.add(chan)};
 }
 static void set_tables(rptq_kv_cache::Tensor& t, const TensorTables& at, const uint8_t* base)
 {
     t.quant = reinterpret_cast<const float2*>(base + at.quant);
     t.value = reinterpret_cast<const float2*>(base + at.value);
+    t.centre = base + at.centre;
+    t.rest = reinterpret_cast<const float2*>(base + at.rest);
     t.pos = reinterpret_cast<const uint16_t*>(base + at.pos);
     t.chan = reinterpret_cast<const int32_t*>(base + at.chan);
 }

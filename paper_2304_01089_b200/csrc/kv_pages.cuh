@@ -28,6 +28,8 @@ struct rptq_kv_cache {
         int64_t row_bytes = 0, slab_bytes = 0, page_bytes = 0;
         const float2* quant = nullptr;     // [H * 32 nu] {inv_s, bits of z - 0x4B400000}; pads give code 0
         const float2* value = nullptr;     // [H * 32 nu] {s, (float) z}
+        const uint8_t* centre = nullptr;   // [H * 32 nu] z, or the code nearest to it: what sums of codes are counted from
+        const float2* rest = nullptr;      // [H * 32 nu] {s, (float) (z - centre)}
         const uint16_t* pos = nullptr;     // [C] position of the channel in a code row of the layout
         const int32_t* chan = nullptr;     // [K_pad] channel at the position, -1 at pads
     } k, v;
