@@ -453,8 +453,8 @@ int rptq_kv_cache_read(const rptq_kv_cache_t* cache, const void* k_pages, const 
  *               nothing is kept in it between calls. Calls that may overlap on the GPU need a workspace each
  * An entry outside 0 .. n_pages - 1 records RPTQ_ERR_BAD_SLOT in the status word and its keys are left out. What the slots behind a
  * sequence's last key hold does not matter. A query that is not finite, or so large that qk_scale |Q s^K| passes 2^108, gives NaN. A
- * probability is held to 2^-27 of the largest among the up to some thousand keys that are worked on together: what keys with smaller ones
- * would add up to is lost. n_seq, n_q_heads <= 65535,
+ * probability is rounded to a multiple of 2^-29 of the largest among the at most 1024 keys that are worked on together, so that
+ * a sum of probabilities is off by less than 2^-20 of itself, however long the sequence is. n_seq, n_q_heads <= 65535,
  * table_width * page_size <= 2^30; n_seq * n_q_heads * (table_width * page_size / 32 + 5) < 2^30.
  */
 int64_t rptq_attention_paged_workspace_bytes(const rptq_kv_cache_t* cache, int n_q_heads);

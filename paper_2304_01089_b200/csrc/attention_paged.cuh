@@ -10,9 +10,10 @@
 //     are finished) and never waits for another group;
 //   - of a pair whose keys are shared by several groups each leaves a partial output in the workspace, and the one that comes last
 //     joins them, in their order: a result does not depend on the order in which groups finish;
-//   - softmax with a running reference: P = 2^(S - ref) with a whole number ref. It moves only when a score passes it, and then to
+//   - softmax with a running reference: P = 2^(S - ref) with a whole number ref. It moves when a score passes it, and then to
 //     HEAD above the tile's maximum, so that nearly all tiles need no maximum and no scaling; moving by whole
-//     numbers scales by exact powers of two;
+//     numbers scales by exact powers of two. After RUN_TILES tiles it begins anew, higher or lower: probabilities are integers, and lose
+//     what lies 2^-30 below the largest of those that have a reference in common;
 //   - K's scale of a channel multiplies the query, V's the result, so neither product has clusters in it (the zero points of K shift all
 //     scores of a row alike). The query becomes integers of 31 bits with one exponent per head, four signed bytes in four
 //     columns of mma.sync m16n8k32 (u8 codes x s8 bytes, exact): two query heads fill the eight columns. Of 4-bit codes the packed word itself
@@ -56,10 +57,15 @@ constexpr int WHOLE_TILES = 10;                // those of at most so many where
                                                // The groups decide, because only they know the lengths: long calls pay 0.3 to 0.6 us for it)
 constexpr int MANY_PARTS = 32;                 // more parts of a pair than these are joined in two levels
 constexpr int MAX_TRIES = 1 << 14;             // (every failed one is another group's success, of which there are a few per part)
-constexpr float HEAD = 4.0f;                   // how far above the largest score a moved reference lies, in powers of two
+constexpr float HEAD = 2.0f;                   // how far above the largest score a moved reference lies, in powers of two: room for the next, taken from the
+                                               // resolution of the probabilities. (8 x 2011 keys 4: 24.77 us, 2: 24.77, 1: 24.91; 3 bits 34.8, 35.4, 35.9)
 constexpr float NO_REF = -0x1p127f;
 constexpr float MAX_UNIT = 0x1p80f;            // of the integers that scores are: a score is less than 2^46 of them, and stays above NO_REF
-constexpr int FLUSH_TILES = 1000;              // 32 keys x 255 x 255 a tile stay below 2^31 in 32-bit sums for 1032 tiles
+constexpr int RUN_TILES = 32;                  // tiles that have a reference in common at most: what the largest key's distance costs the others is then
+                                               // bounded by 1024 keys, however many a group has. (Emptying the integers that often costs a long share
+                                               // less than 1 %: 64 sequences of up to 8000 keys, 16 heads, 82.3 and 82.5 us. 32 keys x 255 x 255
+                                               // a tile would pass 31 bits after 1032)
+constexpr float ONE = 4294967040.0f;           // a probability of 1 relative to its reference: the largest float that is a 32-bit integer
 
 constexpr int SMEM_MAX = 227 * 1024;           // of a block
 constexpr int STAGES = 2;                      // of a group's ring. (Three, more of the cache under way: 2 to 4 % slower; four: 5 %)
@@ -345,7 +351,7 @@ paged_kernel(const Params p)
 
     // ---- per pair
     uint32_t qb[KQ * KI][2];
-    float coef = 0.f, ref = NO_REF;                        // of query head t4 >> 1
+    float coef = 0.f, ref = NO_REF, sum_ref = NO_REF;      // of query head t4 >> 1; ref: of the integers, sum_ref: of the floating sums
     int O[NM][4], L[4];
     float F[NB][4][2], Fl = 0.f;                           // sums that were taken out of the integers; my two of the four digits
     int since = 0, n_heads = 0;
@@ -464,7 +470,7 @@ paged_kernel(const Params p)
 #pragma unroll
         for (int i = 0; i < UN; i += 4) *reinterpret_cast<uint32_t*>(zeros + 32 * i + 4 * lane) = zero_words[i / 4];
         __syncwarp();
-        ref = NO_REF;
+        ref = sum_ref = NO_REF;
 #pragma unroll
         for (int m = 0; m < NM; ++m)
 #pragma unroll
@@ -478,11 +484,12 @@ paged_kernel(const Params p)
         Fl = 0.f;
         since = 0;
     };
-    // The integers move into the 32-bit floating sums, times f. The two digits are joined in floating point: a sum may have 31 bits.
+    // The integers move into the 32-bit floating sums, both relative to the larger of their references from there on. The two digits are joined in floating point: a sum may have 31 bits.
     // The floating sums are of code - zero point (of one outside the codes: less the nearest code), the subtraction still exact: in sums of the
     // codes the outputs, which are means of values around zero, would be differences of far larger numbers.
-    auto flush = [&](float f) {
-        const float w0 = weight, w1 = 256.0f * weight;
+    auto flush = [&]() {
+        const float top = fmaxf(ref, sum_ref), f = ex2(fmaxf(sum_ref - top, -1000.0f)), w0 = weight * ex2(fmaxf(ref - top, -1000.0f)), w1 = 256.0f * w0;
+        sum_ref = top;
         if constexpr (BV == 3) {
             // operand k of a half of a unit is row k & 1 of product k >> 1: of A byte e c0, c0 + 8 c1, all of it; of C byte i c0, c0 + 8 c1, and the
             // single bits on top
@@ -515,7 +522,7 @@ paged_kernel(const Params p)
 #pragma unroll
                 for (int n = 0; n < 16; ++n) {
                     float& x = F[2 * j + (n >> 3)][n & 3][(n >> 2) & 1];
-                    x = f * (x + __fmaf_rn(w1, (float)v[1][n], w0 * (float)v[0][n]));
+                    x = __fmaf_rn(f, x, __fmaf_rn(w1, (float)v[1][n], w0 * (float)v[0][n]));
                 }
             }
         } else {
@@ -533,14 +540,14 @@ paged_kernel(const Params p)
                     o[i] -= (int)((word >> (8 * byte)) & 255u) * (BV == 4 && i >= 2 ? 16 * L[i & 1] : L[i & 1]);
                 }
 #pragma unroll
-                for (int r = 0; r < 2; ++r) F[m >> 2][m & 3][r] = f * (F[m >> 2][m & 3][r] + __fmaf_rn(w1, (float)o[2 * r + 1], w0 * (float)o[2 * r]));
+                for (int r = 0; r < 2; ++r) F[m >> 2][m & 3][r] = __fmaf_rn(f, F[m >> 2][m & 3][r], __fmaf_rn(w1, (float)o[2 * r + 1], w0 * (float)o[2 * r]));
             }
         }
 #pragma unroll
         for (int m = 0; m < NM; ++m)
 #pragma unroll
             for (int i = 0; i < 4; ++i) O[m][i] = 0;
-        Fl = f * (Fl + __fmaf_rn(w1, (float)L[1], w0 * (float)L[0]));
+        Fl = __fmaf_rn(f, Fl, __fmaf_rn(w1, (float)L[1], w0 * (float)L[0]));
 #pragma unroll
         for (int i = 0; i < 4; ++i) L[i] = 0;
         since = 0;
@@ -603,20 +610,21 @@ paged_kernel(const Params p)
                 if (half * SLAB + g8 + 8 * (t4 & 1) >= keys || ((gone >> half) & 1u)) S[half] = -INFINITY;
         }
         // ---------------------------------------------------------------- probabilities relative to the reference
-        if (__any_sync(0xffffffffu, fmaxf(S[0], S[1]) > ref) || since == FLUSH_TILES) {
+        if (__any_sync(0xffffffffu, fmaxf(S[0], S[1]) > ref) || since == RUN_TILES) {
             float m = fmaxf(S[0], S[1]);
             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
 #pragma unroll
             for (int o = 4; o < 32; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-            const float to = m > ref ? ceilf(m) + HEAD : ref;
-            if (since > 0) flush(ex2(fmaxf(ref - to, -1000.0f)));             // (nothing is there at a pair's first tile)
-            ref = to;
+            const float to = fmaxf(ceilf(m) + HEAD, NO_REF);
+            const bool anew = m > ref || since == RUN_TILES;                   // (the other query head's reference may stay)
+            if (since > 0) flush();                                            // (nothing is there at a pair's first tile)
+            if (anew) ref = to;
         }
         ++since;
         // (S - ref first: a whole number added to the exponent before would be rounded with the score)
 #pragma unroll
         for (int half = 0; half < 2; ++half)
-            scratch[(half * WARP_Q + (t4 >> 1)) * SLAB + g8 + 8 * (t4 & 1)] = __float2uint_rn(ex2(S[half] - ref) * 2147483648.0f);
+            scratch[(half * WARP_Q + (t4 >> 1)) * SLAB + g8 + 8 * (t4 & 1)] = __float2uint_rn(ex2(S[half] - ref) * ONE);
         __syncwarp();
         uint32_t pb[2];                                        // operand B of the second product: byte g8 & 3 of four keys
 #pragma unroll
@@ -679,7 +687,7 @@ paged_kernel(const Params p)
         const float2* val = p.val_v + (int64_t)h * nu * 32;
         const int pitch = part_pitch(nu);
         auto part_of = [&](int of, bool begins, int q) { return p.parts + (int64_t)(((of * 2 + begins) * warps + warp) * WARP_Q + q) * pitch; };
-        flush(1.0f);
+        flush();
         float l = Fl + __shfl_xor_sync(0xffffffffu, Fl, 1);
         // a query that is not finite has no sum; nor has a pair none of whose pages exist, which gives zeros
         if (isnan(coef)) l = coef;
@@ -687,7 +695,7 @@ paged_kernel(const Params p)
         const int q = t4 >> 1;
         const bool mine = q < n_heads && (t4 & 1) == 0;
         float* part = part_of(me, first_t == 0, q);
-        if (!complete && mine && g8 == 0) *reinterpret_cast<float2*>(part) = make_float2(ref, l);
+        if (!complete && mine && g8 == 0) *reinterpret_cast<float2*>(part) = make_float2(sum_ref, l);
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
             if (!EXACT && BV != 3 && 2 * b >= nu) break;
