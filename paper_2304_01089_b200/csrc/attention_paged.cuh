@@ -336,7 +336,7 @@ paged_kernel(const Params p)
                 }
                 if (++slab_i == slabs_per_page) { slab_i = 0; ++page_i; }
             }
-            if ((missing & 3u) && p.status) *p.status = RPTQ_ERR_BAD_SLOT;
+            if ((missing & 3u) && lane == 0) record_bad_slot(p.status);
             ++in.t;
             if (--in.n == 0) {
                 next_pair(p, pairs, share == 0, n_groups, end, in);
@@ -747,7 +747,7 @@ paged_kernel(const Params p)
                     else if (atomicCAS(at, seen, p.mark + 1) == seen) before = p.mark;
                 }
                 last = before == p.mark + (unsigned)(count - 1);
-                if ((before & ~0xFFFFull) != p.mark && p.status) *p.status = RPTQ_ERR_DEVICE_TIMEOUT;
+                if ((before & ~0xFFFFull) != p.mark && p.status) atomicExch(p.status, RPTQ_ERR_DEVICE_TIMEOUT);
                 if (last) *reinterpret_cast<volatile unsigned long long*>(at) = p.mark;
             }
             if (!__shfl_sync(0xffffffffu, last, 0)) return;

@@ -57,7 +57,7 @@ __device__ __forceinline__ bool find_slot(const Params& p, int token, int64_t& p
     const int64_t slot = p.slots[token];
     if (slot < 0) return false;
     if (slot >= p.n_slots) {
-        if (p.status) *p.status = RPTQ_ERR_BAD_SLOT;
+        record_bad_slot(p.status);
         return false;
     }
     page = page_of(slot, p.P);
@@ -107,7 +107,7 @@ __device__ __forceinline__ Window find_groups(const Params& p, const Side& s, in
     bool leads = false;
     if (i < end && slot >= 0) {
         if (slot >= p.n_slots) {
-            if (p.status) *p.status = RPTQ_ERR_BAD_SLOT;
+            record_bad_slot(p.status);
         } else {
             leads = in_four == 0 || before != slot - 1;
             const int64_t page = page_of(slot, p.P);

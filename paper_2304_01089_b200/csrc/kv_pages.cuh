@@ -86,6 +86,13 @@ __device__ __forceinline__ uint32_t code_of_three(Byte byte, int at)
     return (byte(h, i) >> 6) | (((byte(2, 2 * h + (i >> 1)) >> (6 + (i & 1))) & 1u) << 2);
 }
 
+// A slot or page outside its pool. A time-out that is recorded already stays: it says that an output is undefined, this only that something was
+// left out.
+__device__ __forceinline__ void record_bad_slot(int* status)
+{
+    if (status) atomicCAS(status, RPTQ_OK, RPTQ_ERR_BAD_SLOT);
+}
+
 // Where a slot's slab begins in the pool: page, head, slab of the page.
 __host__ __device__ __forceinline__ int64_t slab_offset(int64_t page, int64_t page_bytes, int head, int slabs_per_page, int slab, int64_t slab_bytes)
 {
