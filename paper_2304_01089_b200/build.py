@@ -1,10 +1,16 @@
-"""Compile the CUDA sources under csrc/ into librptq.so (sm_100a only), and calls.cpp, which hands PyTorch's tensors to it, into _calls.so; in-tree."""
+"""Compile the CUDA sources under csrc/ into librptq.so (sm_100a only), and calls.cpp, which hands PyTorch's tensors to it, into _calls.so; in-tree.
+
+librptq.so needs nvcc alone. _calls.so is built where a PyTorch for CUDA is installed, for that PyTorch and Python: without it `binding.KvCache`
+raises, everything else works."""
 from __future__ import annotations
 
 import glob
+import importlib.metadata
 import importlib.util
 import os
+import shutil
 import subprocess
+import sys
 import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -29,19 +35,46 @@ def dependencies():
     return sources() + [f for pattern in headers for f in sorted(glob.glob(pattern))]
 
 
-def needs_build() -> bool:
-    if not os.path.exists(LIB) or not os.path.exists(CALLS):
+def _older(target: str, files) -> bool:
+    return not os.path.exists(target) or any(os.path.getmtime(f) > os.path.getmtime(target) for f in files)
+
+
+def _torch():
+    """The installed PyTorch's folder; None if there is none, or one without CUDA."""
+    spec = importlib.util.find_spec("torch")
+    at = spec.submodule_search_locations[0] if spec and spec.submodule_search_locations else None
+    return at if at and os.path.exists(os.path.join(at, "lib", "libc10_cuda.so")) else None
+
+
+def _calls_tag() -> str:
+    """What _calls.so is built for; it carries this text."""
+    return f"rptq calls for torch {importlib.metadata.version('torch')}, {sys.implementation.cache_tag};"
+
+
+def library_is_stale() -> bool:
+    return _older(LIB, [f for f in dependencies() if not f.endswith(".cpp")])
+
+
+def calls_are_stale() -> bool:
+    if _torch() is None:
+        return False
+    if _older(CALLS, [os.path.join(CSRC, "calls.cpp"), os.path.join(ROOT, "include", "rptq.h")]):
         return True
-    t = min(os.path.getmtime(LIB), os.path.getmtime(CALLS))
-    return any(os.path.getmtime(d) > t for d in dependencies())
+    with open(CALLS, "rb") as f:
+        return _calls_tag().encode() not in f.read()
+
+
+def needs_build() -> bool:
+    return library_is_stale() or calls_are_stale()
 
 
 def build_calls() -> str:
     """calls.cpp against the headers of the installed PyTorch; it finds librptq.so beside itself."""
-    torch = os.path.join(importlib.util.find_spec("torch").submodule_search_locations[0])
-    cuda = os.environ.get("CUDA_HOME", "/usr/local/cuda")
+    torch = _torch()
+    cuda = os.environ.get("CUDA_HOME") or os.path.dirname(os.path.dirname(os.path.realpath(shutil.which("nvcc") or "/usr/local/cuda/bin/nvcc")))
     tmp = CALLS + f".tmp{os.getpid()}"
-    subprocess.run(["g++", "-shared", "-fPIC", "-O2", "-std=c++17", "-Wall", "-I", os.path.join(ROOT, "include"), "-I", sysconfig.get_paths()["include"],
+    subprocess.run(["g++", "-shared", "-fPIC", "-O2", "-std=c++17", "-Wall", f'-DRPTQ_CALLS_TAG="{_calls_tag()}"',
+                    "-I", os.path.join(ROOT, "include"), "-I", sysconfig.get_paths()["include"],
                     "-I", os.path.join(torch, "include"), "-I", os.path.join(torch, "include", "torch", "csrc", "api", "include"),
                     "-I", os.path.join(cuda, "include"), os.path.join(CSRC, "calls.cpp"), "-o", tmp, "-L", HERE, "-l:librptq.so", "-Wl,-rpath,$ORIGIN",
                     "-L", os.path.join(torch, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"], check=True)
@@ -50,17 +83,16 @@ def build_calls() -> str:
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    if not force and not needs_build():
-        return LIB
-    tmp = LIB + f".tmp{os.getpid()}"
-    cmd = ["nvcc", "-shared", "--threads", str(os.cpu_count() or 1), *NVCC_FLAGS, *(["-Xptxas", "-v"] if verbose else []),
-           *sources(), "-o", tmp, "-lgomp"]
-    subprocess.run(cmd, check=True)
-    os.replace(tmp, LIB)
-    build_calls()
+    if force or library_is_stale():
+        tmp = LIB + f".tmp{os.getpid()}"
+        cmd = ["nvcc", "-shared", "--threads", str(os.cpu_count() or 1), *NVCC_FLAGS, *(["-Xptxas", "-v"] if verbose else []),
+               *sources(), "-o", tmp, "-lgomp"]
+        subprocess.run(cmd, check=True)
+        os.replace(tmp, LIB)
+    if calls_are_stale() or (force and _torch() is not None):
+        build_calls()
     return LIB
 
 
 if __name__ == "__main__":
-    import sys
     print(build(force=True, verbose="-v" in sys.argv))

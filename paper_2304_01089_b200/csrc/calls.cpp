@@ -216,6 +216,7 @@ PyMethodDef methods[] = {
     {"attention_paged", fast(attention_paged), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
+extern "C" __attribute__((used, visibility("default"))) const char rptq_calls_tag[] = RPTQ_CALLS_TAG;     // (build.py looks for it)
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -375,3 +375,32 @@ def test_a_run_of_parts_is_read_by_all_lanes_before_its_sum_replaces_the_first()
     assert load < join.index("__syncwarp();", load) < store
     branch = join[:store].rindex("if (++i < count) continue;")             # uniform: every lane comes to the synchronisation
     assert branch < join.index("__syncwarp();", load)
+
+
+def test_the_library_is_built_without_pytorch(monkeypatch):
+    """librptq.so needs nvcc alone; the module that hands PyTorch's tensors to it is left out where there is no PyTorch, or one without CUDA."""
+    import importlib.util
+    import types
+    ran = []
+    monkeypatch.setattr(lib_build.subprocess, "run", lambda cmd, **kw: ran.append(cmd[0]))
+    monkeypatch.setattr(lib_build.os, "replace", lambda a, b: None)
+    real = importlib.util.find_spec
+    for torch in (None, types.SimpleNamespace(submodule_search_locations=[os.path.join(ROOT, "tests")])):
+        monkeypatch.setattr(importlib.util, "find_spec", lambda name, *a: torch if name == "torch" else real(name, *a))
+        ran.clear()
+        assert lib_build.build(force=True) == lib_build.LIB and ran == ["nvcc"]
+        assert not lib_build.calls_are_stale()
+
+
+def test_a_calls_module_of_another_pytorch_is_stale(monkeypatch):
+    import importlib.metadata
+    lib_build.build()
+    assert not lib_build.needs_build()
+    real = importlib.metadata.version
+    monkeypatch.setattr(importlib.metadata, "version", lambda name: "1.0.0+other" if name == "torch" else real(name))
+    assert lib_build.needs_build()
+    ran = []
+    monkeypatch.setattr(lib_build.subprocess, "run", lambda cmd, **kw: ran.append(cmd))
+    monkeypatch.setattr(lib_build.os, "replace", lambda a, b: None)
+    lib_build.build()                                                       # and is built again, the library is not
+    assert [c[0] for c in ran] == ["g++"] and any("1.0.0+other" in a for a in ran[0])
