@@ -30,7 +30,7 @@ constexpr int THREADS = 128;
 // One tensor (K or V) of a call.
 struct Side {
     int bits;
-    int64_t row_bytes, slab_bytes, page_bytes;
+    int64_t slab_bytes, page_bytes;
     const float2 *quant, *value;
     const uint16_t* pos;
     const int32_t* chan;
@@ -569,7 +569,7 @@ static int make_params(const rptq_kv_cache_t* c, const void* k, int64_t ldk, con
     for (int t = 0; t < 2; ++t) {
         const rptq_kv_cache::Tensor& x = t ? c->v : c->k;
         Side& s = p->side[t];
-        s.bits = x.bits; s.row_bytes = x.row_bytes; s.slab_bytes = x.slab_bytes; s.page_bytes = x.page_bytes;
+        s.bits = x.bits; s.slab_bytes = x.slab_bytes; s.page_bytes = x.page_bytes;
         s.quant = x.quant; s.value = x.value; s.pos = x.pos; s.chan = x.chan; s.n_units_row = x.K_pad / 32;
         s.pages = static_cast<uint8_t*>(const_cast<void*>(t ? v_pages : k_pages));
         s.rows = const_cast<void*>(t ? v : k);
