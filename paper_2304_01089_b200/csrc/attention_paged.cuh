@@ -9,7 +9,8 @@
 //     each; it has a ring of tiles in shared memory (cp.async, to the end of its share: the next pair's tiles travel while this one's
 //     are finished) and never waits for another group;
 //   - of a pair whose keys are shared by several groups each leaves a partial output in the workspace, and the one that comes last
-//     joins them, in their order: a result does not depend on the order in which groups finish;
+//     joins them, in their order (of more than MANY_PARTS in two levels: the last of a run of parts joins the run, the last of the runs their
+//     sums): a result does not depend on the order in which groups finish;
 //   - softmax with a running reference: P = 2^(S - ref) with a whole number ref. It moves when a score passes it, and then to
 //     HEAD above the tile's maximum, so that nearly all tiles need no maximum and no scaling; moving by whole
 //     numbers scales by exact powers of two. After RUN_TILES tiles it begins anew, higher or lower: probabilities are integers, and lose
@@ -19,14 +20,16 @@
 //     columns of mma.sync m16n8k32 (u8 codes x s8 bytes, exact): two query heads fill the eight columns. Of 4-bit codes the packed word itself
 //     is an operand: its bytes are 16 hi + lo, so with the integer y of hi's channel counted in units 16 times larger and x - y in place
 //     of lo's x, x lo + 16 y hi = (x - y) lo + y (16 hi + lo) takes one AND for eight codes; 3-bit pages are made for the same (kv_pages.cuh). A
-//     channel's query is off by at most 2^-27 of the head's largest (3 bits: 2^-25): no more than 32-bit sums lose;
+//     channel's query, whose largest lies in [2^29, 2^30), is off by at most 2^-26 of the head's largest (a step of 16; 8 bits: 2^-30; 3
+//     bits, a step of 64: 2^-24);
 //   - probabilities as unsigned 32-bit integers, four bytes in four columns, V^T as operand A. The sums are exact, and keys behind the last
 //     one or on a page that does not exist have P = 0 whatever bytes lie there. (Codes as fp16 with eight query heads in a warp's eight
 //     columns took three instructions per four codes to convert, twice the registers, and 50 us where this takes 24 us: 64 sequences of
 //     up to 1337 keys, 32 query heads on 8 cached ones, 8 bits.)
-// Measured: 72 heads of 128 channels, eight sequences of up to 2011 keys (10904 in all), 4 bits: 24.5 us, of which finding the share, the
-// first tiles, parts and join take 8 and the rest runs at 5.8 TB/s; one sequence of 65553 keys, 32 heads: 52.5 us, 5.1 TB/s over all; 3 bits, 96
-// heads, sixteen sequences of up to 1700 keys: 35.2 us, 3.2 TB/s, where instructions bound it too.
+// Measured: 72 heads of 128 channels, eight sequences of up to 2011 keys (10859 in all), 4 bits: 24.9 us, of which finding the share, the
+// first tiles, parts and join take 8 and the rest runs at 5.8 TB/s; one sequence of 65553 keys, 32 heads: 53.3 us, 5.0 TB/s over all; 3 bits, 96
+// heads, sixteen sequences of up to 1700 keys: 35.6 us, 3.2 TB/s: there a warp's tile is 474 instructions one behind the other, and with 2.8 warps a
+// scheduler neither memory nor the issue slots (48 %) are full.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>

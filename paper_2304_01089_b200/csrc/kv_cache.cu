@@ -6,7 +6,7 @@
 // bytes of V that one token owns lie four apart, but four tokens' bytes of a word are 16 in a row (a 4 x 4 transposition in registers). One
 // token alone writes its bytes one by one.
 // The next group's loads are under way while a group is worked on. Rows of values are read and written past the caches (they are
-// used once; with the default policy the longest timed case took 77 us).
+// used once; with the default policy writing and reading 4096 tokens took 77 us instead of 72).
 // Measured (4096 tokens, 72 heads of 128 channels, 4 bits, fp16, caches cold): writing 41 us, 4.6 TB/s; reading back 34 us, 5.6 TB/s.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -405,7 +405,7 @@ __device__ __forceinline__ void read_rows(const Params& p, const Side& s, int fi
 
 // A warp takes a chunk of 256 channels of K or V (blockIdx.y) and a window of the tokens; the four warps of a block take neighbouring
 // chunks. Six blocks per SM write (80 registers; rows of fp32 four, 128), eight read (64). (Parts as long as make all warps resident at once, K's and V's at the same
-// time, were 15 % slower: 90 us against 77 for the longest timed case.)
+// time, were 15 % slower when that was tried, before the rows passed the caches by: 90 us against 77 for writing and reading 4096 tokens.)
 template <class T> constexpr int rows_blocks_per_sm(bool write) { return !write ? 8 : sizeof(T) == 4 ? 4 : 6; }
 template <class T, bool WRITE>
 __global__ void __launch_bounds__(THREADS, rows_blocks_per_sm<T>(WRITE)) rows_kernel(const Params p)
@@ -514,8 +514,8 @@ __global__ void __launch_bounds__(THREADS) code_rows_kernel(const Params p)
     }
 }
 
-// Tokens per warp: as many as leave WARPS_PER_SM warps for every SM. (Measured with 16, 32, 64, 128: 83, 83, 87, 96 us for the longest timed
-// case, 8.7, 9.3, 9.4, 9.3 for the shortest with several tokens.)
+// Tokens per warp: as many as leave WARPS_PER_SM warps for every SM. (Measured with 8, 16, 32, 64: one token and 16 rows back for eight sequences 6.9,
+// 7.1, 8.7, 8.7 us; chunks of 333 tokens for three 15.6, 11.5, 12.8, 16.3; 2011 rows of 3 bits 18.2, 18.2, 18.2, 20.7; 4096 tokens 68 with each.)
 constexpr int WARPS_PER_SM = 16;
 template <class T, bool WRITE>
 static int launch_values(Params& p, int n_sm, cudaStream_t st)
