@@ -48,7 +48,11 @@ def _torch():
 
 def _calls_tag() -> str:
     """What _calls.so is built for; it carries this text."""
-    return f"rptq calls for torch {importlib.metadata.version('torch')}, {sys.implementation.cache_tag};"
+    try:
+        torch = importlib.metadata.version("torch")
+    except importlib.metadata.PackageNotFoundError:                         # built from source, without an installation's record
+        torch = _torch()
+    return f"rptq calls for torch {torch}, {sys.implementation.cache_tag};"
 
 
 def library_is_stale() -> bool:

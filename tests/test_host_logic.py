@@ -404,3 +404,9 @@ def test_a_calls_module_of_another_pytorch_is_stale(monkeypatch):
     monkeypatch.setattr(lib_build.os, "replace", lambda a, b: None)
     lib_build.build()                                                       # and is built again, the library is not
     assert [c[0] for c in ran] == ["g++"] and any("1.0.0+other" in a for a in ran[0])
+
+    def unknown(name):
+        raise importlib.metadata.PackageNotFoundError(name)
+
+    monkeypatch.setattr(importlib.metadata, "version", unknown)             # a PyTorch without an installation's record
+    assert lib_build.needs_build()
