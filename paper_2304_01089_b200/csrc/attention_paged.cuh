@@ -487,7 +487,8 @@ paged_kernel(const Params p)
         Fl = 0.f;
         since = 0;
     };
-    // The integers move into the 32-bit floating sums, both relative to the larger of their references from there on. The two digits are joined in floating point: a sum may have 31 bits.
+    // The integers move into the 32-bit floating sums, both relative to the larger of their references from there on. The two digits are joined in
+    // floating point: one's sum has up to 26 bits, the other counts 2^8 times as much.
     // The floating sums are of code - zero point (of one outside the codes: less the nearest code), the subtraction still exact: in sums of the
     // codes the outputs, which are means of values around zero, would be differences of far larger numbers.
     auto flush = [&]() {

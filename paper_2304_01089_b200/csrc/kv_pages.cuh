@@ -2,8 +2,8 @@
 // attention_paged.cu (which attends over them).
 //
 // A page holds page_size keys of every head: [head][slab of 16 keys]. A head's channels are kept in their own order, rounded up to
-// units of 32 (what pads hold does not matter: their integers of the query are 0, their outputs are not stored). The reorder's clusters do not appear: attention multiplies the query by the channels' scales first,
-// so that one sum over all channels takes the place of a sum per cluster, and a cluster need not start at a unit of its own. (Four clusters
+// units of 32 (what pads hold does not matter: their integers of the query are 0, their outputs are not stored). The reorder's
+// clusters do not appear: attention multiplies the query by the channels' scales first, so that one sum over all channels takes the place of a sum per cluster, and a cluster need not start at a unit of its own. (Four clusters
 // of 128 channels take 4 units here and about 5.5 in a row of the padded layout.)
 // 32 codes of a unit are BITS words in both tensors: with 4 and 8 bits those of the library's packed format. With 3 bits a byte holds two codes
 // and two single bits, so that AND and the byte itself bring them apart as far as a product needs (c0, c0 + 8 c1, c0 + 8 c1 + 64 b; the
